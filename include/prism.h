@@ -53,6 +53,7 @@ extern "C" {
 #define PRISM_MAX_CANDS    4096  /* candidates per call */
 #define PRISM_MAX_CLUSTERS 8
 #define PRISM_MAX_SEQ      8192  /* tokens per (query + candidate) sequence */
+#define PRISM_MAX_STEP     1048576  /* rows of one step over a paged cache (prism_page_shape.n_tokens) */
 #define PRISM_N_KINDS      6     /* kernel kinds timed in prism_report */
 
 /* fates written to prism_report.ev_fate (Sec. 4.1) */
@@ -300,6 +301,79 @@ int prism_op_dequantize_w4(const void *blob, int32_t N, int32_t K, int32_t dtype
 int prism_op_attention(int32_t dtype, const void *QK, const void *Vt, int64_t vt_stride,
                        const int32_t *cu_seqlens_host, const int32_t *vt_col0_host, int32_t n_seqs,
                        int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void *out, void *stream);
+
+/* ---- Paged K/V cache -----------------------------------------------------------------------------------------------
+ * For callers that keep keys and values between calls: documents read in chunks, sequences that grow by a few tokens.  The cache is
+ * a pool of pages; sequence s finds the keys of positions i * page_size .. (i + 1) * page_size - 1 in page table[s][i].  A step is
+ * prism_op_page_plan once, then for every layer prism_op_qkv_finish_paged (which appends) and prism_op_attention_paged (which reads).
+ * None of the three allocates, synchronises or reads device values on the host, so a step can be captured into a graph and replayed
+ * on new lengths of the same shape.  Lengths, tables, slots and free pages are device values and are not checked by the host: what
+ * they ask for beyond the buffers given is left out, as stated at each call, and nothing outside the buffers is touched. */
+
+/* One pool of pages.  Page p of the keys starts at K + p * page_stride (in values of dtype; likewise V) and holds
+ * [n_kv_heads][page_size][head_dim] values.  K and V may interleave in one allocation.  Pages 16-byte aligned; page_size 16, 32, 64,
+ * 128 or 256; head_dim 64 or 128, with dtype FP32 also 32; n_pages * page_size < 2^31. */
+typedef struct {
+  void   *K, *V;                      /* [device] */
+  int64_t page_stride;                /* >= n_kv_heads * page_size * head_dim */
+  int32_t dtype;                      /* PRISM_DTYPE_*: of keys, values, queries and outputs */
+  int32_t n_kv_heads, head_dim, page_size, n_pages;
+} prism_kv_cache;
+
+/* Shape of a step: what the host knows of it.  n_tokens is the number of rows of the step's buffers: at least the sequences' fresh
+ * tokens together, more where the batch is padded; rows behind the last sequence belong to nobody. */
+typedef struct {
+  int32_t n_seqs;                     /* 0..PRISM_MAX_CANDS */
+  int32_t n_tokens;                   /* 0..PRISM_MAX_STEP */
+  int32_t n_q_heads, n_kv_heads;      /* up to 128 query heads per KV head, up to 256 KV heads */
+  int32_t page_size, n_pages;         /* as in prism_kv_cache */
+  int32_t max_pages;                  /* row length of the page table; max_pages * page_size <= 2^29 */
+  int32_t window;                     /* > 0: a token sees the last `window` positions up to its own; 0: all */
+} prism_page_shape;
+
+/* Layout of a step, from the sequences' lengths.  cached, fresh [n_seqs]: tokens of each sequence in the cache before the step, and
+ * tokens that the step brings (negative ones count as 0); its rows are sequence by sequence, row cu[s] + i at position
+ * cached[s] + i.  All pointers [device].
+ *   table [n_seqs][max_pages], in and out: entries from ceil(cached / page_size) on that the step reaches get new pages, in order of
+ *     sequence, then position, off the end of free_pages[0 .. *n_free) (at most free_cap entries); the others are not written.
+ *     *n_free_left = free pages left; it may be n_free itself.  An entry for which there is no page left becomes -1.
+ *   cu [n_seqs + 1], pos [n_tokens], slot [n_tokens], out: slot = page * page_size + position % page_size; -1 for a token without a
+ *     page (none left, behind the table's end, or a table entry outside the pool) and for rows behind the last sequence (pos 0).
+ *   status [4], out, may be NULL: rows of the sequences, pages taken, pages missing, fresh tokens behind row n_tokens (left out).
+ *   plan [prism_page_plan_bytes], out, 16-byte aligned: the attention's work list, for this shape.
+ * The call depends on its inputs alone: repeated with the same ones (say for another window, n_free_left apart from n_free) it gives
+ * the same pages.  Sequences may share pages that are full; the caller keeps count of them.  With shape->n_seqs = 0 every row is
+ * behind the last sequence.  prism_page_plan_bytes: -1 for a bad shape. */
+int64_t prism_page_plan_bytes(const prism_page_shape *shape);
+int prism_op_page_plan(const prism_page_shape *shape, const int32_t *cached, const int32_t *fresh, int32_t *table,
+                       const int32_t *free_pages, int32_t free_cap, const int32_t *n_free, int32_t *n_free_left, int32_t *cu,
+                       int32_t *pos, int32_t *slot, int32_t *status, void *plan, void *stream);
+
+/* prism_op_qkv_finish for a paged cache, in one pass: per-head RMSNorm (optional; gains in the cache's type) and rotate-half RoPE on q
+ * and k, each rounded once to the cache's type; q to rows of Q, k and v to their slots.  QKV: T rows of (nq + 2 nkv) * head_dim
+ * values, fp32 or the cache's type (qkv_dtype), qkv_stride apart; Q: rows q_stride apart (strides multiples of 4, pointers aligned
+ * to 4 values).  pos, slot [T] [device] as prism_op_page_plan writes them: pos >= 0 without an upper bound (angles are evaluated in
+ * fp64); where slot is outside [0, n_pages * page_size) only q is written.  Two rows of one slot leave either's values.  Q must not
+ * overlap QKV.  NaN stays NaN; half saturates. */
+int prism_op_qkv_finish_paged(const prism_kv_cache *cache, int32_t qkv_dtype, const void *QKV, int64_t qkv_stride, int32_t T,
+                              const int32_t *pos, const int32_t *slot, int32_t n_q_heads, const void *q_gain, const void *k_gain,
+                              float eps, float rope_base, int32_t qk_norm, void *Q, int64_t q_stride, void *stream);
+
+/* Attention of the step's tokens over the cache, which holds their own keys and values already.  A query at position p sees the keys
+ * of its sequence at positions k <= p (with a window: p - window < k) that have a page in the pool; scores are
+ *   s = scale q.k (scale 0: 1 / sqrt(head_dim)),  softcap > 0: s = softcap tanh(s / softcap),  slopes: s -= slopes[head] (p - k),
+ * softmax over the keys seen, times V.  A query that sees no key gives zeros; rows behind the last sequence are not written.  Keys
+ * and values that a query does not see never reach its result, whatever they hold (NaN and infinities included).
+ *   shape, plan, table: those of prism_op_page_plan (with a plan of another shape nothing is written).  Q, out: n_tokens rows of
+ *   n_q_heads * head_dim values of the cache's type, q_stride / out_stride apart (rows 16-byte aligned); out may be Q itself.
+ *   slopes [n_q_heads] fp32 [device] or NULL.
+ *   workspace [device], 16-byte aligned, prism_attention_paged_workspace bytes (-1 for a bad shape): partial results of queries whose
+ *   keys are split over several workgroups.  Contents need no initialisation; calls that overlap need one each.
+ * The order of a row's sums depends on the shape and on all lengths of the step, not on timing: same inputs, same bits. */
+int64_t prism_attention_paged_workspace(const prism_page_shape *shape, int32_t head_dim);
+int prism_op_attention_paged(const prism_page_shape *shape, const prism_kv_cache *cache, const void *plan, const int32_t *table,
+                             const void *Q, int64_t q_stride, float scale, float softcap, const float *slopes, void *out,
+                             int64_t out_stride, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Intermediate scorer (Sec. 4.1): for each sequence c, the last token's state through the final RMSNorm and
  * the yes/no head: scores[c] = z . w_yes - z . w_no.  last_row[c] = row of that token in X (NULL: row c). */

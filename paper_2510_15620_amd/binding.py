@@ -24,7 +24,9 @@ MAX_CANDS, MAX_CLUSTERS, MAX_SEQ = 4096, 8, 8192
 
 EXPORTS = ["prism_create", "prism_select", "prism_set_forced_keep", "prism_destroy", "prism_strerror",
            "prism_last_error", "prism_op_embed", "prism_op_rmsnorm", "prism_op_gemm", "prism_op_qkv_finish", "prism_op_qkv_project", "prism_w4_bytes", "prism_op_quantize_w4", "prism_op_dequantize_w4",
-           "prism_op_attention", "prism_op_score", "prism_op_route", "prism_op_route_static", "prism_op_compact", "prism_op_topk", "prism_vt_column_of_key"]
+           "prism_op_attention", "prism_op_score", "prism_op_route", "prism_op_route_static", "prism_op_compact", "prism_op_topk", "prism_vt_column_of_key",
+           "prism_page_plan_bytes", "prism_op_page_plan", "prism_op_qkv_finish_paged", "prism_attention_paged_workspace",
+           "prism_op_attention_paged"]
 
 
 class PrismError(RuntimeError):
@@ -55,6 +57,15 @@ class prism_options(C.Structure):
                 ("n_clusters", C.c_int32), ("mode", C.c_int32), ("chunk_cands", C.c_int32), ("hbm_cap_bytes", C.c_int64),
                 ("stream", C.c_void_p), ("operand", C.c_int32), ("offload_hidden", C.c_int32), ("embed_cache_rows", C.c_int32), ("stream_slots", C.c_int32),
                 ("no_query_sharing", C.c_int32), ("single_pass_checks", C.c_int32)]
+
+
+class prism_kv_cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("page_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("dtype", "n_kv_heads", "head_dim", "page_size", "n_pages")]
+
+
+class prism_page_shape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "n_tokens", "n_q_heads", "n_kv_heads", "page_size", "n_pages", "max_pages", "window")]
 
 
 class prism_report(C.Structure):
@@ -113,6 +124,14 @@ def lib() -> C.CDLL:
         _lib.prism_w4_bytes.argtypes = [i32, i32]
         _lib.prism_op_quantize_w4.argtypes = [vp, i32, i32, vp, vp]
         _lib.prism_op_dequantize_w4.argtypes = [vp, i32, i32, i32, vp, vp]
+        i64, shape, cache = C.c_int64, C.POINTER(prism_page_shape), C.POINTER(prism_kv_cache)
+        _lib.prism_page_plan_bytes.restype = i64
+        _lib.prism_page_plan_bytes.argtypes = [shape]
+        _lib.prism_op_page_plan.argtypes = [shape, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        _lib.prism_op_qkv_finish_paged.argtypes = [cache, i32, vp, i64, i32, vp, vp, i32, vp, vp, f32, f32, i32, vp, i64, vp]
+        _lib.prism_attention_paged_workspace.restype = i64
+        _lib.prism_attention_paged_workspace.argtypes = [shape, i32]
+        _lib.prism_op_attention_paged.argtypes = [shape, cache, vp, vp, vp, i64, f32, f32, vp, vp, i64, vp, i64, vp]
     return _lib
 
 
@@ -365,3 +384,118 @@ def op_compact(X_src, X_dst, src_start, dst_start, length):
 
 def op_topk(scores, K, out_pos, out_scores):
     _check(lib().prism_op_topk(_ptr(scores), scores.numel(), K, _ptr(out_pos), _ptr(out_scores), _stream()))
+
+
+# ---- paged K/V cache ----------------------------------------------------------------------------------------------------
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise PrismError(EINVAL, what)
+
+
+def _ints(t, n: int, device: int, what: str) -> int:
+    """Address of a dense int32 device tensor of at least n values."""
+    import torch
+    _need(t.dtype is torch.int32 and t.numel() >= n and t.is_contiguous() and t.get_device() == device,
+          f"{what}: a dense int32 tensor of {n} values on the current device")
+    return t.data_ptr()
+
+
+def _rows(t, n: int, width: int, dtype, device: int, what: str):
+    """Address and row stride of an [n, width] device tensor whose rows are dense."""
+    _need(t.dim() == 2 and t.shape[0] == n and t.shape[1] == width and t.dtype is dtype and (width < 2 or t.stride(1) == 1) and
+          t.get_device() == device, f"{what}: [{n}, {width}] of {dtype}, rows dense, on the current device")
+    return t.data_ptr(), t.stride(0) if n > 1 else width
+
+
+def _device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+class KVCache:
+    """A pool of pages: K and V [n_pages, n_kv_heads, page_size, head_dim] device tensors of one dtype.  Pages are dense; the stride
+    from page to page is free, and the same for both (K and V may be views into one allocation)."""
+
+    def __init__(self, K, V):
+        import torch
+        _need(K.dim() == 4 and K.shape == V.shape and K.dtype is V.dtype and K.is_cuda and K.device == V.device, "KVCache: K and V alike")
+        n, heads, size, hd = K.shape
+        _need(K.dtype in (torch.float32, torch.bfloat16, torch.float16), "KVCache: fp32, bf16 or half")
+        for t in (K, V):
+            _need(all(t.shape[i] < 2 or t.stride(i) == s for i, s in ((1, size * hd), (2, hd), (3, 1))), "KVCache: pages have to be dense")
+        stride = K.stride(0) if n > 1 else heads * size * hd
+        _need(n < 2 or V.stride(0) == stride, "KVCache: K and V have the same stride between pages")
+        self.K, self.V, self.dtype, self.device = K, V, K.dtype, K.get_device()
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = n, heads, size, hd
+        self._c = prism_kv_cache(K.data_ptr(), V.data_ptr(), stride, _dt(K), heads, hd, size, n)
+        self._ref = C.byref(self._c)
+
+
+class PagePlan:
+    """The shape of a step (see prism_page_shape) and the device buffer of its plan.  Filled by op_page_plan, read by
+    op_attention_paged; may be filled again for another step of the same shape."""
+
+    def __init__(self, n_seqs: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, page_size: int, n_pages: int, max_pages: int,
+                 window: int = 0):
+        import torch
+        self._c = prism_page_shape(n_seqs, n_tokens, n_q_heads, n_kv_heads, page_size, n_pages, max_pages, window)
+        self._ref = C.byref(self._c)
+        size = int(lib().prism_page_plan_bytes(self._ref))
+        if size < 0:
+            raise PrismError(EINVAL, lib().prism_last_error().decode())
+        self.n_seqs, self.n_tokens, self.n_q_heads, self.max_pages = n_seqs, n_tokens, n_q_heads, max_pages
+        self.buffer = torch.zeros(size, dtype=torch.uint8, device="cuda")
+        self.device = self.buffer.get_device()
+
+
+def op_page_plan(plan: PagePlan, cached, fresh, table, free_pages, n_free, n_free_left, cu, pos, slot, status=None):
+    """cached, fresh [n_seqs]; table [n_seqs, max_pages]; free_pages [any]; n_free, n_free_left [1]; cu [n_seqs + 1]; pos, slot
+    [n_tokens]; status [4] or None: int32 device tensors."""
+    d, n, T = _device(), plan.n_seqs, plan.n_tokens
+    _need(plan.device == d, "op_page_plan: the plan is on another device than the current one")
+    _check(lib().prism_op_page_plan(
+        plan._ref, _ints(cached, n, d, "cached"), _ints(fresh, n, d, "fresh"), _ints(table, n * plan.max_pages, d, "table"),
+        _ints(free_pages, 0, d, "free_pages"), free_pages.numel(), _ints(n_free, 1, d, "n_free"), _ints(n_free_left, 1, d, "n_free_left"),
+        _ints(cu, n + 1, d, "cu"), _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"),
+        0 if status is None else _ints(status, 4, d, "status"), plan.buffer.data_ptr(), _stream()))
+
+
+def op_qkv_finish_paged(QKV, pos, slot, cache: KVCache, q_gain, k_gain, eps, base, qk_norm, Q):
+    """QKV [T, (nq + 2 nkv) * hd] fp32 or in the cache's dtype -> Q [T, nq * hd] and the cache's slots."""
+    import torch
+    d, hd, nkv = _device(), cache.head_dim, cache.n_kv_heads
+    T, nq = QKV.shape[0], Q.shape[1] // hd
+    _need(cache.device == d, "op_qkv_finish_paged: the cache is on another device than the current one")
+    x, x_stride = _rows(QKV, T, (nq + 2 * nkv) * hd, torch.float32 if QKV.dtype is torch.float32 else cache.dtype, d, "QKV")
+    q, q_stride = _rows(Q, T, nq * hd, cache.dtype, d, "Q")
+    if qk_norm:
+        for g in (q_gain, k_gain):
+            _need(g is not None and g.dtype is cache.dtype and g.numel() == hd and g.is_contiguous() and g.get_device() == d,
+                  "op_qkv_finish_paged: gains of head_dim values in the cache's dtype")
+    _check(lib().prism_op_qkv_finish_paged(cache._ref, _dt(QKV), x, x_stride, T, _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"), nq,
+                                           _ptr(q_gain), _ptr(k_gain), eps, base, int(qk_norm), q, q_stride, _stream()))
+
+
+def attention_paged_workspace(plan: PagePlan, cache: KVCache):
+    """A workspace for op_attention_paged: calls that may overlap need one each."""
+    import torch
+    size = int(lib().prism_attention_paged_workspace(plan._ref, cache.head_dim))
+    if size < 0:
+        raise PrismError(EINVAL, lib().prism_last_error().decode())
+    return torch.empty(size, dtype=torch.uint8, device="cuda")
+
+
+def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace, scale: float = 0.0, softcap: float = 0.0, slopes=None):
+    """Q, out [n_tokens, n_q_heads * hd] in the cache's dtype; table as op_page_plan left it; slopes [n_q_heads] fp32 or None."""
+    import torch
+    d, T, width = _device(), plan.n_tokens, plan.n_q_heads * cache.head_dim
+    _need(plan.device == d and cache.device == d and workspace.get_device() == d, "op_attention_paged: tensors on another device than the current one")
+    q, q_stride = _rows(Q, T, width, cache.dtype, d, "Q")
+    o, o_stride = _rows(out, T, width, cache.dtype, d, "out")
+    if slopes is not None:
+        _need(slopes.dtype is torch.float32 and slopes.numel() == plan.n_q_heads and slopes.is_contiguous() and slopes.get_device() == d,
+              "op_attention_paged: slopes of n_q_heads fp32 values")
+    _check(lib().prism_op_attention_paged(plan._ref, cache._ref, plan.buffer.data_ptr(), _ints(table, plan.n_seqs * plan.max_pages, d, "table"),
+                                          q, q_stride, scale, softcap, _ptr(slopes), o, o_stride, workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _stream()))

@@ -87,6 +87,13 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// (cos, sin)(pos * base^(-2 i / hd)) of rotation pair i of half = hd / 2, evaluated in fp64 and rounded once
+__device__ __forceinline__ float2 rotation(int pos, int i, int half, double log2_base) {
+  const double theta = exp2(-(double)i / (double)half * log2_base);
+  const double a = (double)pos * theta;
+  return make_float2((float)cos(a), (float)sin(a));
+}
+
 // ---- launchers (each validates shapes, launches on `s`, never synchronises) -------------------
 int launch_embed(const int32_t *tokens, int T, const void *table, int hidden, int dtype, float *X, hipStream_t s);
 int launch_rmsnorm(const float *X, const void *gain, int T, int hidden, float eps, int dtype, void *out, hipStream_t s);

@@ -150,12 +150,6 @@ int launch_rmsnorm(const float *X, const void *gain, int T, int hidden, float ep
 // ------------------------------------------------------------------------------------------------
 // RoPE table, evaluated in fp64 and rounded once: (cos, sin)(pos * base^(-2 i / hd)) at tab[pos * half + i], or, transposed,
 // at tab[i * n_pos + pos] (the layout the fused q/k/v epilogue reads: consecutive tokens of a sequence are then neighbours).
-__device__ __forceinline__ float2 rotation(int pos, int i, int half, double log2_base) {
-  const double theta = exp2(-(double)i / (double)half * log2_base);
-  const double a = (double)pos * theta;
-  return make_float2((float)cos(a), (float)sin(a));
-}
-
 __global__ void rope_table_kernel(float2 *tab, int n_pos, int half, double log2_base, int transposed) {
   const int idx = blockIdx.x * blockDim.x + threadIdx.x;
   if (idx >= n_pos * half) return;

@@ -1,0 +1,92 @@
+// Shared declarations of the operators on a paged K/V cache (paged_plan.hip, paged_finish.hip, attn_paged.hip, attn_paged_fp32.hip).
+#pragma once
+
+#include "common.h"
+
+namespace prism {
+
+// A plan is one device buffer: header, one record per sequence, work items of the attention, blocks whose keys were split.
+//
+// A block is up to 128 query rows of one (sequence, KV head): whole tokens, the G query heads of the KV head side by side, so that
+// every head grouping fills the matrix cores' rows and K/V are read once for all of them.  An item is a block and a run of 64-key
+// tiles.  A sequence's blocks are all cut into the same number of runs, n_parts: its longest block's tiles over the launch's
+// tiles per item, which are the total over kPlanItems / n_kv_heads, and kPlanMinTiles at least.  So
+//   items <= kPlanItems / n_kv_heads + blocks,   items of cut blocks < 2 kPlanItems / n_kv_heads,
+// which is what bounds a launch's grid and the room for partial results without the host knowing a length.
+static const int kPlanRows = 128;        // query rows of a block
+static const int kPlanTile = 64;         // keys of a tile
+static const int kPlanItems = 1024;      // items wanted over all KV heads: two workgroups on each of 256 compute units, twice
+static const int kPlanMinTiles = 4;      // tiles of an item at least, where that leaves fewer items than wanted
+static const int kJoinRows = 16;         // query rows whose parts one workgroup joins
+static const int kPlanMagic = 0x70616765;
+static const int kGroupMax = kPlanRows;  // query heads per KV head
+
+struct PlanHeader {
+  int32_t magic;
+  prism_page_shape shape;
+  int32_t n_items, n_joins;
+  int32_t pad[5];
+};
+static_assert(sizeof(PlanHeader) == 64, "one cache-line half");
+struct PlanSeq { int32_t row0, rows, cached, has, page0, n_parts, item0, part0, join0, pad[3]; };  // page0: rank of its first new page
+struct PlanItem { int32_t seq, row0, n_tok, pos0, tile0, tile1, part0, pad; };        // part0: first partial row, -1: the block is whole
+struct PlanJoin { int32_t row0, n_tok, part0, n_parts, step, pad[3]; };                 // part j of its rows: from part0 + j * step on
+
+// tokens of a join and of a block, which holds whole joins
+__host__ __device__ inline int plan_join_tokens(const prism_page_shape &s) {
+  const int g = s.n_q_heads / s.n_kv_heads;
+  return g < kJoinRows ? kJoinRows / g : 1;
+}
+__host__ __device__ inline int plan_block_tokens(const prism_page_shape &s) {
+  const int t = plan_join_tokens(s);
+  return kPlanRows / (s.n_q_heads / s.n_kv_heads) / t * t;
+}
+__host__ __device__ inline int plan_goal(const prism_page_shape &s) { return (kPlanItems + s.n_kv_heads - 1) / s.n_kv_heads; }
+__host__ __device__ inline int64_t plan_blocks(const prism_page_shape &s) { return s.n_tokens / plan_block_tokens(s) + s.n_seqs; }
+__host__ __device__ inline int64_t plan_items(const prism_page_shape &s) { return plan_blocks(s) + plan_goal(s); }
+__host__ __device__ inline int64_t plan_joins(const prism_page_shape &s) {
+  const int t = plan_join_tokens(s);
+  const int64_t by_tokens = s.n_tokens / t + s.n_seqs, by_blocks = (int64_t)plan_goal(s) * (plan_block_tokens(s) / t);
+  return by_tokens < by_blocks ? by_tokens : by_blocks;    // fewer than goal blocks are cut
+}
+// partial rows of a KV head: fewer than 2 goal parts of up to kPlanRows rows, and every row in goal + 1 parts at most
+__host__ __device__ inline int64_t plan_part_rows(const prism_page_shape &s) {
+  const int64_t by_parts = 2 * (int64_t)plan_goal(s) * kPlanRows;
+  const int64_t by_rows = (int64_t)s.n_tokens * (s.n_q_heads / s.n_kv_heads) * (plan_goal(s) + 1);
+  return by_parts < by_rows ? by_parts : by_rows;
+}
+__host__ __device__ inline size_t plan_items_at(const prism_page_shape &s) { return sizeof(PlanHeader) + (size_t)s.n_seqs * sizeof(PlanSeq); }
+__host__ __device__ inline size_t plan_joins_at(const prism_page_shape &s) { return plan_items_at(s) + (size_t)plan_items(s) * sizeof(PlanItem); }
+__host__ __device__ inline size_t plan_bytes(const prism_page_shape &s) { return plan_joins_at(s) + (size_t)plan_joins(s) * sizeof(PlanJoin); }
+
+__host__ __device__ inline bool same_shape(const prism_page_shape &a, const prism_page_shape &b) {
+  return a.n_seqs == b.n_seqs && a.n_tokens == b.n_tokens && a.n_q_heads == b.n_q_heads && a.n_kv_heads == b.n_kv_heads &&
+         a.page_size == b.page_size && a.n_pages == b.n_pages && a.max_pages == b.max_pages && a.window == b.window;
+}
+int check_page_shape(const prism_page_shape *s, const char *who);
+int check_kv_cache(const prism_kv_cache *c, const char *who);
+
+// 16-bit results of these operators: as from_f32, but NaN stays NaN
+template <typename T> __device__ __forceinline__ T round_to(float v) { return from_f32<T>(v); }
+template <> __device__ __forceinline__ f16 round_to<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }
+
+// What an attention launch reads and writes.  Partial results of part row i and KV head h: values at O[(i * n_kv + h) * hd], running
+// maximum and sum of weights at ml[i * n_kv + h].  unit: from a difference of the maxima to the exponent of 2 that its weight has.
+struct PagedAttn {
+  prism_page_shape shape;
+  const PlanHeader *plan;
+  const PlanItem *items;
+  const PlanJoin *joins;
+  const int32_t *table;
+  const void *Q, *K, *V;
+  void *out;
+  const float *slopes;
+  float *part_O;
+  float2 *part_ml;
+  int64_t q_stride, out_stride, page_stride;
+  float scale, softcap, unit;
+  int page_shift;
+};
+int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s);
+
+}  // namespace prism
