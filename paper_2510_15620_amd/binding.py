@@ -393,24 +393,30 @@ def _need(ok: bool, what: str):
         raise PrismError(EINVAL, what)
 
 
-def _ints(t, n: int, device: int, what: str) -> int:
-    """Address of a dense int32 device tensor of at least n values."""
+def _ints(device: int, **tensors):
+    """Addresses of dense int32 device tensors; name=(tensor, values that it has to hold)."""
     import torch
-    _need(t.dtype is torch.int32 and t.numel() >= n and t.is_contiguous() and t.get_device() == device,
-          f"{what}: a dense int32 tensor of {n} values on the current device")
-    return t.data_ptr()
+    i32, out = torch.int32, []
+    for t, n in tensors.values():
+        if t.dtype is not i32 or t.numel() < n or not t.is_contiguous() or t.get_device() != device:
+            name = next(k for k, v in tensors.items() if v[0] is t)
+            raise PrismError(EINVAL, f"{name}: a dense int32 tensor of {n} values on the current device")
+        out.append(t.data_ptr())
+    return out
 
 
 def _rows(t, n: int, width: int, dtype, device: int, what: str):
     """Address and row stride of an [n, width] device tensor whose rows are dense."""
-    _need(t.dim() == 2 and t.shape[0] == n and t.shape[1] == width and t.dtype is dtype and (width < 2 or t.stride(1) == 1) and
-          t.get_device() == device, f"{what}: [{n}, {width}] of {dtype}, rows dense, on the current device")
+    if t.shape != (n, width) or t.dtype is not dtype or t.get_device() != device or (t.stride(1) != 1 and width > 1):
+        raise PrismError(EINVAL, f"{what}: [{n}, {width}] of {dtype}, rows dense, on the current device")
     return t.data_ptr(), t.stride(0) if n > 1 else width
 
 
-def _device() -> int:
+def _here():
+    """Current device and its current stream."""
     import torch
-    return torch.cuda.current_device()
+    d = torch.cuda.current_device()
+    return d, torch._C._cuda_getCurrentRawStream(d)          # the stream's handle without making a Stream object
 
 
 class KVCache:
@@ -448,33 +454,38 @@ class PagePlan:
         self.buffer = torch.zeros(size, dtype=torch.uint8, device="cuda")
         self.device = self.buffer.get_device()
 
+    @property
+    def address(self):
+        return self.buffer.data_ptr()
+
 
 def op_page_plan(plan: PagePlan, cached, fresh, table, free_pages, n_free, n_free_left, cu, pos, slot, status=None):
     """cached, fresh [n_seqs]; table [n_seqs, max_pages]; free_pages [any]; n_free, n_free_left [1]; cu [n_seqs + 1]; pos, slot
     [n_tokens]; status [4] or None: int32 device tensors."""
-    d, n, T = _device(), plan.n_seqs, plan.n_tokens
+    (d, stream), n, T = _here(), plan.n_seqs, plan.n_tokens
     _need(plan.device == d, "op_page_plan: the plan is on another device than the current one")
-    _check(lib().prism_op_page_plan(
-        plan._ref, _ints(cached, n, d, "cached"), _ints(fresh, n, d, "fresh"), _ints(table, n * plan.max_pages, d, "table"),
-        _ints(free_pages, 0, d, "free_pages"), free_pages.numel(), _ints(n_free, 1, d, "n_free"), _ints(n_free_left, 1, d, "n_free_left"),
-        _ints(cu, n + 1, d, "cu"), _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"),
-        0 if status is None else _ints(status, 4, d, "status"), plan.buffer.data_ptr(), _stream()))
+    cached, fresh, table, pages, *out = _ints(
+        d, cached=(cached, n), fresh=(fresh, n), table=(table, n * plan.max_pages), free_pages=(free_pages, 0), n_free=(n_free, 1),
+        n_free_left=(n_free_left, 1), cu=(cu, n + 1), pos=(pos, T), slot=(slot, T), **({} if status is None else {"status": (status, 4)}))
+    _check(lib().prism_op_page_plan(plan._ref, cached, fresh, table, pages, free_pages.numel(), *out, *(() if status is not None else (0,)),
+                                    plan.address, stream))
 
 
 def op_qkv_finish_paged(QKV, pos, slot, cache: KVCache, q_gain, k_gain, eps, base, qk_norm, Q):
     """QKV [T, (nq + 2 nkv) * hd] fp32 or in the cache's dtype -> Q [T, nq * hd] and the cache's slots."""
     import torch
-    d, hd, nkv = _device(), cache.head_dim, cache.n_kv_heads
+    (d, stream), hd, nkv = _here(), cache.head_dim, cache.n_kv_heads
     T, nq = QKV.shape[0], Q.shape[1] // hd
     _need(cache.device == d, "op_qkv_finish_paged: the cache is on another device than the current one")
     x, x_stride = _rows(QKV, T, (nq + 2 * nkv) * hd, torch.float32 if QKV.dtype is torch.float32 else cache.dtype, d, "QKV")
+    at, slots = _ints(d, pos=(pos, T), slot=(slot, T))
     q, q_stride = _rows(Q, T, nq * hd, cache.dtype, d, "Q")
     if qk_norm:
         for g in (q_gain, k_gain):
             _need(g is not None and g.dtype is cache.dtype and g.numel() == hd and g.is_contiguous() and g.get_device() == d,
                   "op_qkv_finish_paged: gains of head_dim values in the cache's dtype")
-    _check(lib().prism_op_qkv_finish_paged(cache._ref, _dt(QKV), x, x_stride, T, _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"), nq,
-                                           _ptr(q_gain), _ptr(k_gain), eps, base, int(qk_norm), q, q_stride, _stream()))
+    _check(lib().prism_op_qkv_finish_paged(cache._ref, DTYPE_FP32 if QKV.dtype is torch.float32 else cache._c.dtype, x, x_stride, T, at, slots, nq,
+                                           _ptr(q_gain), _ptr(k_gain), eps, base, int(qk_norm), q, q_stride, stream))
 
 
 def attention_paged_workspace(plan: PagePlan, cache: KVCache):
@@ -489,13 +500,14 @@ def attention_paged_workspace(plan: PagePlan, cache: KVCache):
 def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace, scale: float = 0.0, softcap: float = 0.0, slopes=None):
     """Q, out [n_tokens, n_q_heads * hd] in the cache's dtype; table as op_page_plan left it; slopes [n_q_heads] fp32 or None."""
     import torch
-    d, T, width = _device(), plan.n_tokens, plan.n_q_heads * cache.head_dim
+    (d, stream), T, width = _here(), plan.n_tokens, plan.n_q_heads * cache.head_dim
     _need(plan.device == d and cache.device == d and workspace.get_device() == d, "op_attention_paged: tensors on another device than the current one")
     q, q_stride = _rows(Q, T, width, cache.dtype, d, "Q")
     o, o_stride = _rows(out, T, width, cache.dtype, d, "out")
     if slopes is not None:
         _need(slopes.dtype is torch.float32 and slopes.numel() == plan.n_q_heads and slopes.is_contiguous() and slopes.get_device() == d,
               "op_attention_paged: slopes of n_q_heads fp32 values")
-    _check(lib().prism_op_attention_paged(plan._ref, cache._ref, plan.buffer.data_ptr(), _ints(table, plan.n_seqs * plan.max_pages, d, "table"),
-                                          q, q_stride, scale, softcap, _ptr(slopes), o, o_stride, workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _stream()))
+    pages, = _ints(d, table=(table, plan.n_seqs * plan.max_pages))
+    _need(workspace.is_contiguous(), "op_attention_paged: a dense workspace")
+    _check(lib().prism_op_attention_paged(plan._ref, cache._ref, plan.address, pages, q, q_stride, scale, softcap, _ptr(slopes), o, o_stride,
+                                          workspace.data_ptr(), workspace.nbytes, stream))

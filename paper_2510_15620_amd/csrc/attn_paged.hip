@@ -121,8 +121,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
 
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
+  const PlanItem it = a.items[item];                          // within the list's room, whatever it holds: asked for with the header
   if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || item >= a.plan->n_items) return;
-  const PlanItem it = a.items[item];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = it.n_tok * G, window = a.shape.window;
   const int cap_keys = a.shape.max_pages << a.page_shift;
@@ -610,82 +610,88 @@ void attention_paged_16_kernel(const PagedAttn a) {
 }
 
 // Rows whose keys were split: out = sum_j w_j O_j / sum_j w_j l_j with w_j = 2^(unit (m_j - m)), HD / 4 lanes per row.  A row's parts are dealt to
-// 2, 4 or 8 (all of the workgroup) such groups of lanes, which meet in LDS.
+// 1, 2, 4 or 8 such groups of lanes, which meet in LDS, and a group requests eight parts together.  Bound by memory latency.
 template <typename OT, int HD>
 __global__ __launch_bounds__(2 * HD) void paged_join_kernel(const PagedAttn a) {
-  constexpr int L = HD / 4, N = 8;                            // lanes of a row, groups of lanes
+  constexpr int L = HD / 4, N = 8, U = 8;                     // lanes of a row, groups of lanes, parts of a group under way together
   struct alignas(4 * sizeof(OT)) Out { OT v[4]; };
   __shared__ __align__(16) float lO[N][HD];
   __shared__ float2 lml[N];
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
-  const int kvh = blockIdx.x % nkv, join = blockIdx.x / nkv;
-  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || join >= a.plan->n_joins) return;
-  const PlanJoin jn = a.joins[join];
-  const int group = threadIdx.x / L, d = (threadIdx.x % L) * 4;
-  const int deal = jn.n_parts > 4 ? 8 : jn.n_parts > 2 ? 4 : 2, own = group % deal, rows = jn.n_tok * G, at_once = N / deal;
-  for (int r0 = 0; r0 < rows; r0 += at_once) {
-    const int r = r0 + group / deal < rows ? r0 + group / deal : rows - 1;
-    float m = -INFINITY, sum = 0.f;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    // the running maximum of a group's parts; four parts' loads at a time
-    for (int j0 = own; j0 < jn.n_parts; j0 += 4 * deal) {
-      float2 x[4];
-      f32x4 y[4];
+  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape)) return;
+  const int n = a.plan->n_joins * nkv;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int kvh = i % nkv;
+    const PlanJoin jn = a.joins[i / nkv];
+    const int group = threadIdx.x / L, d = (threadIdx.x % L) * 4;
+    const int deal = jn.n_parts > 4 * U ? 8 : jn.n_parts > 2 * U ? 4 : jn.n_parts > U ? 2 : 1, own = group % deal, rows = jn.n_tok * G, at_once = N / deal;
+    for (int r0 = blockIdx.y * at_once; r0 < rows; r0 += gridDim.y * at_once) {
+      const int r = r0 + group / deal < rows ? r0 + group / deal : rows - 1;
+      float m = -INFINITY, sum = 0.f;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int j0 = own; j0 < jn.n_parts; j0 += U * deal) {
+        float2 x[U];
+        f32x4 y[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int j = j0 + u * deal;
-        const int64_t at = (int64_t)(jn.part0 + (j < jn.n_parts ? j : own) * jn.step + r) * nkv + kvh;
-        x[u] = a.part_ml[at];
-        y[u] = *reinterpret_cast<const f32x4 *>(a.part_O + at * HD + d);
-        if (j >= jn.n_parts) x[u] = make_float2(-INFINITY, 0.f);
+        for (int u = 0; u < U; ++u) {
+          const int j = j0 + u * deal;
+          const int64_t at = (int64_t)(jn.part0 + (j < jn.n_parts ? j : own) * jn.step + r) * nkv + kvh;
+          x[u] = a.part_ml[at];
+          y[u] = *reinterpret_cast<const f32x4 *>(a.part_O + at * HD + d);
+          if (j >= jn.n_parts) x[u] = make_float2(-INFINITY, 0.f);
+        }
+        float mx = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) mx = fmaxf(mx, x[u].x);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        const float f0 = __builtin_amdgcn_exp2f((m - ref) * a.unit);
+        m = mx;
+        sum *= f0;
+        v *= f0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (x[u].x == -INFINITY) continue;                    // a part without keys has nothing
+          const float f = __builtin_amdgcn_exp2f((x[u].x - ref) * a.unit);
+          sum += f * x[u].y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += f * y[u][e];
+        }
       }
-      const float mx = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), m), ref = mx == -INFINITY ? 0.f : mx;
-      const float f0 = __builtin_amdgcn_exp2f((m - ref) * a.unit);
-      m = mx;
-      sum *= f0;
-      v *= f0;
+      *reinterpret_cast<f32x4 *>(&lO[group][d]) = v;
+      if (d == 0) lml[group] = make_float2(m, sum);
+      __syncthreads();
+      if (group < at_once && r0 + group < rows) {               // this group's lanes: row r0 + group
+        const int first = group * deal, row = r0 + group;
+        float mx = -INFINITY;
+        for (int j = 0; j < deal; ++j) mx = fmaxf(mx, lml[first + j].x);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float total = 0.f;
+        f32x4 w = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < deal; ++j) {
+          const float2 x = lml[first + j];
+          if (x.x == -INFINITY) continue;
+          const float f = __builtin_amdgcn_exp2f((x.x - ref) * a.unit);
+          const f32x4 y = *reinterpret_cast<const f32x4 *>(&lO[first + j][d]);
+          total += f * x.y;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (x[u].x == -INFINITY) continue;                    // a part without keys has nothing
-        const float f = __builtin_amdgcn_exp2f((x[u].x - ref) * a.unit);
-        sum += f * x[u].y;
+          for (int e = 0; e < 4; ++e) w[e] += f * y[e];
+        }
+        const int t = row / G, h = kvh * G + row - t * G;
+        Out o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += f * y[u][e];
+        for (int e = 0; e < 4; ++e) o.v[e] = round_to<OT>(total == 0.f ? 0.f : w[e] / total);
+        *reinterpret_cast<Out *>((OT *)a.out + (int64_t)(jn.row0 + t) * a.out_stride + (int64_t)h * HD + d) = o;
       }
+      __syncthreads();
     }
-    *reinterpret_cast<f32x4 *>(&lO[group][d]) = v;
-    if (d == 0) lml[group] = make_float2(m, sum);
-    __syncthreads();
-    if (group < at_once && r0 + group < rows) {               // this group's lanes: row r0 + group
-      const int first = group * deal, row = r0 + group;
-      float mx = -INFINITY;
-      for (int j = 0; j < deal; ++j) mx = fmaxf(mx, lml[first + j].x);
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      float total = 0.f;
-      f32x4 w = {0.f, 0.f, 0.f, 0.f};
-      for (int j = 0; j < deal; ++j) {
-        const float2 x = lml[first + j];
-        if (x.x == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f((x.x - ref) * a.unit);
-        const f32x4 y = *reinterpret_cast<const f32x4 *>(&lO[first + j][d]);
-        total += f * x.y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] += f * y[e];
-      }
-      const int t = row / G, h = kvh * G + row - t * G;
-      Out o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o.v[e] = round_to<OT>(total == 0.f ? 0.f : w[e] / total);
-      *reinterpret_cast<Out *>((OT *)a.out + (int64_t)(jn.row0 + t) * a.out_stride + (int64_t)h * HD + d) = o;
-    }
-    __syncthreads();
   }
 }
 
 template <typename OT, int HD>
 static int launch_join(const PagedAttn &a, hipStream_t s) {
-  const int64_t joins = plan_joins(a.shape) * a.shape.n_kv_heads;
-  paged_join_kernel<OT, HD><<<(int)joins, 2 * HD, 0, s>>>(a);
+  const int64_t joins = plan_joins(a.shape) * a.shape.n_kv_heads;     // there may be far fewer
+  // few joins: they have few rows and many parts, and the rows go to workgroups of their own
+  paged_join_kernel<OT, HD><<<dim3(joins < 8192 ? joins : 8192, joins < 512 ? 4 : 1), 2 * HD, 0, s>>>(a);
   PRISM_HIP(hipGetLastError());
   return PRISM_OK;
 }

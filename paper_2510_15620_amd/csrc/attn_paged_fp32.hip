@@ -2,8 +2,9 @@
 // arithmetic and operand layout as in attn_fp32.hip: both products transposed, so that a lane owns one row (lane % 16) and the
 // accumulators of S^T are the next contraction's operand; operands straight from memory, one group of 16 keys ahead.
 //
-// A wave takes 16 rows at a time.  Items of more than 32 rows: the waves take turns with the row blocks, each over all keys.  Items
-// of up to 32 rows: all waves take the same rows and every fourth group of keys, and meet in LDS.
+// A wave takes 16 rows.  Items of more than 32 rows: a wave per 16 rows, each over all keys, in two workgroups (the matrix work of an
+// item is 16 times that of the 16-bit types, and a step of short chunks has few items).  Items of up to 32 rows: one workgroup whose
+// waves take the same rows and every fourth group of keys, and meet in LDS.
 #include <type_traits>
 
 #include "paged.h"
@@ -18,10 +19,10 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   __shared__ float2 lml[4][16];
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
-  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || item >= a.plan->n_items) return;
   const PlanItem it = a.items[item];
+  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || item >= a.plan->n_items) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int rows = it.n_tok * G, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
+  const int rows = it.n_tok * G, row_begin = blockIdx.y * 64, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
   const int last = it.pos0 + it.n_tok - 1, limit = last + 1 < cap_keys ? last + 1 : cap_keys;
   const int32_t *const table = a.table + (int64_t)it.seq * a.shape.max_pages;
   const float *const Kh = (const float *)a.K + ((int64_t)kvh * HD << a.page_shift), *const Vh = (const float *)a.V + ((int64_t)kvh * HD << a.page_shift);
@@ -53,10 +54,11 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
     }
   };
   const bool shared = rows <= 32;
+  if (row_begin >= rows) return;
   const int n_groups = (limit + 15) >> 4, g_end = it.tile1 * 4 < n_groups ? it.tile1 * 4 : n_groups;
   const int g_first = it.tile0 * 4 + (shared ? wave : 0), g_step = shared ? 4 : 1;
-  const int blocks = (rows + 15) / 16;
-  for (int rb = shared ? 0 : wave; rb < blocks; rb += shared ? 1 : 4) {
+  const int blocks = ((rows < row_begin + 64 ? rows : row_begin + 64) + 15) / 16;
+  for (int rb = shared ? 0 : row_begin / 16 + wave; rb < blocks; rb += shared ? 1 : 4) {
     const int r = rb * 16 + c < rows ? rb * 16 + c : rows - 1, tok = r / G, head = kvh * G + r - tok * G, pos = it.pos0 + tok;
     const int r_last = rb * 16 + 15 < rows ? rb * 16 + 15 : rows - 1;
     const int b_first = it.pos0 + rb * 16 / G, b_last = it.pos0 + r_last / G;    // positions of the block's first and last row
@@ -228,8 +230,8 @@ int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s) {
   const bool mod = a.softcap > 0.f || a.slopes;
   auto run = [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
-    if (mod) attention_paged_fp32_kernel<NB, true><<<grid, 256, 0, s>>>(a);
-    else attention_paged_fp32_kernel<NB, false><<<grid, 256, 0, s>>>(a);
+    if (mod) attention_paged_fp32_kernel<NB, true><<<dim3(grid, kPlanRows / 64), 256, 0, s>>>(a);
+    else attention_paged_fp32_kernel<NB, false><<<dim3(grid, kPlanRows / 64), 256, 0, s>>>(a);
   };
   if (hd == 32) run(std::integral_constant<int, 2>{});
   else if (hd == 64) run(std::integral_constant<int, 4>{});

@@ -9,23 +9,27 @@ namespace prism {
 //
 // A block is up to 128 query rows of one (sequence, KV head): whole tokens, the G query heads of the KV head side by side, so that
 // every head grouping fills the matrix cores' rows and K/V are read once for all of them.  An item is a block and a run of 64-key
-// tiles.  A sequence's blocks are all cut into the same number of runs, n_parts: its longest block's tiles over the launch's
-// tiles per item, which are the total over kPlanItems / n_kv_heads, and kPlanMinTiles at least.  So
-//   items <= kPlanItems / n_kv_heads + blocks,   items of cut blocks < 2 kPlanItems / n_kv_heads,
+// tiles.  A sequence's blocks are all cut into the same number of runs, by its longest block's tiles.  What a cut costs is the
+// partial results, written and read again in fp32: little for a sequence of up to kPlanNarrow rows, which is cut into runs of the
+// step's tiles over plan_goal (two items for each of the 512 workgroups that the chip holds); as much as four tiles for a block of
+// 128 rows, so those are cut into runs of twice that, and only where they have half as many again.  So per KV head
+//   items <= plan_goal + blocks,   items of cut blocks < 2 plan_goal, their rows < 128 plan_goal,
 // which is what bounds a launch's grid and the room for partial results without the host knowing a length.
 static const int kPlanRows = 128;        // query rows of a block
 static const int kPlanTile = 64;         // keys of a tile
 static const int kPlanItems = 1024;      // items wanted over all KV heads: two workgroups on each of 256 compute units, twice
 static const int kPlanMinTiles = 4;      // tiles of an item at least, where that leaves fewer items than wanted
-static const int kJoinRows = 16;         // query rows whose parts one workgroup joins
+static const int kPlanNarrow = 32;       // rows of a sequence whose keys are cut freely
+static const int kPlanMinWide = 8;       // the same for the others
+static const int kJoinRows = 8;          // query rows whose parts one workgroup joins
 static const int kPlanMagic = 0x70616765;
 static const int kGroupMax = kPlanRows;  // query heads per KV head
 
 struct PlanHeader {
   int32_t magic;
   prism_page_shape shape;
-  int32_t n_items, n_joins;
-  int32_t pad[5];
+  int32_t n_items, n_joins, n_free;       // n_free: free pages before the step
+  int32_t pad[4];
 };
 static_assert(sizeof(PlanHeader) == 64, "one cache-line half");
 struct PlanSeq { int32_t row0, rows, cached, has, page0, n_parts, item0, part0, join0, pad[3]; };  // page0: rank of its first new page
@@ -42,6 +46,8 @@ __host__ __device__ inline int plan_block_tokens(const prism_page_shape &s) {
   return kPlanRows / (s.n_q_heads / s.n_kv_heads) / t * t;
 }
 __host__ __device__ inline int plan_goal(const prism_page_shape &s) { return (kPlanItems + s.n_kv_heads - 1) / s.n_kv_heads; }
+// half of it, but one at least: items of the wide blocks are as long as 1 / plan_wide_goal of all tiles, which is 2 / plan_goal or more
+__host__ __device__ inline int plan_wide_goal(const prism_page_shape &s) { return plan_goal(s) > 1 ? plan_goal(s) / 2 : 1; }
 __host__ __device__ inline int64_t plan_blocks(const prism_page_shape &s) { return s.n_tokens / plan_block_tokens(s) + s.n_seqs; }
 __host__ __device__ inline int64_t plan_items(const prism_page_shape &s) { return plan_blocks(s) + plan_goal(s); }
 __host__ __device__ inline int64_t plan_joins(const prism_page_shape &s) {
@@ -49,9 +55,10 @@ __host__ __device__ inline int64_t plan_joins(const prism_page_shape &s) {
   const int64_t by_tokens = s.n_tokens / t + s.n_seqs, by_blocks = (int64_t)plan_goal(s) * (plan_block_tokens(s) / t);
   return by_tokens < by_blocks ? by_tokens : by_blocks;    // fewer than goal blocks are cut
 }
-// partial rows of a KV head: fewer than 2 goal parts of up to kPlanRows rows, and every row in goal + 1 parts at most
+// Partial rows of a KV head.  Of the tiles, w in wide blocks and n in narrow ones, w + n = 1: fewer than 2 n goal parts of up to
+// kPlanNarrow rows and w goal of up to kPlanRows, so goal kPlanRows at most; and every row is in goal + 1 parts at most.
 __host__ __device__ inline int64_t plan_part_rows(const prism_page_shape &s) {
-  const int64_t by_parts = 2 * (int64_t)plan_goal(s) * kPlanRows;
+  const int64_t by_parts = (int64_t)plan_goal(s) * kPlanRows;
   const int64_t by_rows = (int64_t)s.n_tokens * (s.n_q_heads / s.n_kv_heads) * (plan_goal(s) + 1);
   return by_parts < by_rows ? by_parts : by_rows;
 }

@@ -4,250 +4,263 @@
 // Everything is a sum over the sequences in front: rows, new pages, items.  One workgroup takes those sums (page_plan_kernel: up to
 // four sequences per thread, three scans); what they say about each row and item is then independent work, found by a binary
 // search.  Steps of up to kPlanAlone rows are finished by the same workgroup, larger ones by a second launch of many.
-// Bound by launch and memory latency: a step's bytes are nothing.
+// Bound by launch and memory latency and by the chain of the sums: a step's bytes are nothing.  So there is no division but by shift
+// and multiplication, every wave's load of a value is asked for once, and 64 bits only where a sum needs them.
 #include "paged.h"
 
 namespace prism {
 
-static const int kPlanThreads = 1024;
-static const int kPlanAlone = 4096;      // rows that the summing workgroup lays out itself
+static const int kPlanAlone = 4096;      // rows that the summing workgroup lays out itself, of up to kPlanInLds sequences
+static const int kPlanInLds = 1024;
+
+// x / d for x up to 2^20 and d up to 128: the product's error, x (2^32 / d rounded up - 2^32 / d), stays below 2^32 / d
+struct Divisor {
+  uint32_t d, m;
+  __device__ __forceinline__ int operator()(int x) const { return d == 1 ? x : (int)__umulhi((uint32_t)x, m); }
+};
+static Divisor divisor(int d) { return {(uint32_t)d, (uint32_t)((((uint64_t)1 << 32) + d - 1) / d)}; }
 
 struct PlanArgs {
   prism_page_shape s;
   const int32_t *cached, *fresh;
   int32_t *table;
   const int32_t *free_pages, *n_free;
-  int32_t free_cap;
   int32_t *n_free_left, *cu, *pos, *slot, *status;
-  char *plan;
+  PlanHeader *head;
+  PlanSeq *seqs;
+  PlanItem *items;
+  PlanJoin *joins;
+  Divisor block, join;                    // by the tokens of a block and of a join
+  int free_cap, page_shift, G, goal, wide_goal;
 };
 
-// inclusive sums over the workgroup's threads of three values at once; total: the last thread's
-struct Sums { int64_t a, b, c; };
+// Sums that stop at 2^31 - 1: of terms that are not negative, in any grouping the same
+__device__ __forceinline__ int add_capped(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+
+// sums over the workgroup's threads in front of this one, of three values at once; total: over all of them
+struct Sums { int a, b, c; };
+template <int WAVES>
 __device__ __forceinline__ Sums block_scan(Sums v, Sums *lds, Sums &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t a = __shfl_up(v.a, o, 64), b = __shfl_up(v.b, o, 64), c = __shfl_up(v.c, o, 64);
-    if (lane >= o) { v.a += a; v.b += b; v.c += c; }
+    const int a = __shfl_up(v.a, o, 64), b = __shfl_up(v.b, o, 64), c = __shfl_up(v.c, o, 64);
+    if (lane >= o) { v.a = add_capped(v.a, a); v.b = add_capped(v.b, b); v.c = add_capped(v.c, c); }
   }
   if (lane == 63) lds[wave] = v;
+  v = {__shfl_up(v.a, 1, 64), __shfl_up(v.b, 1, 64), __shfl_up(v.c, 1, 64)};
+  if (lane == 0) v = {0, 0, 0};
   __syncthreads();
   Sums before = {0, 0, 0};
   total = {0, 0, 0};
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const Sums t = lds[w];
-    if (w < wave) { before.a += t.a; before.b += t.b; before.c += t.c; }
-    total.a += t.a; total.b += t.b; total.c += t.c;
+    if (w == wave) before = total;
+    total.a = add_capped(total.a, t.a); total.b = add_capped(total.b, t.b); total.c = add_capped(total.c, t.c);
   }
   __syncthreads();
-  return {v.a + before.a, v.b + before.b, v.c + before.c};
+  return {add_capped(v.a, before.a), add_capped(v.b, before.b), add_capped(v.c, before.c)};
 }
 
 // the last i in [0, n) with first[i] <= x; first[0] = 0
 __device__ __forceinline__ int last_at_or_before(const int32_t *first, int n, int x) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= x) lo = mid; else hi = mid;
-  }
+  int lo = 0;
+  for (int step = 1 << (31 - __builtin_clz(n)); step > 0; step >>= 1)
+    if (lo + step < n && first[lo + step] <= x) lo += step;
   return lo;
 }
 
-// Rows and items that thread `me` of `all` lays out; row0 and item0: the sequences' first ones, in LDS.
-__device__ void lay_out(const PlanArgs &a, const int32_t *row0, const int32_t *item0, int64_t me, int64_t all) {
+// Rows and items that thread `me` of `all` lays out; row0, item0 and seqs of the n sequences, of which total rows and n_items are.
+__device__ __forceinline__ void lay_out(const PlanArgs &a, const int32_t *row0, const int32_t *item0, const PlanSeq *seqs, int total, int n_items,
+                                        int n_free, int me, int all) {
   const prism_page_shape &s = a.s;
-  const PlanHeader *h = reinterpret_cast<const PlanHeader *>(a.plan);
-  const PlanSeq *seqs = reinterpret_cast<const PlanSeq *>(a.plan + sizeof(PlanHeader));
-  PlanItem *items = reinterpret_cast<PlanItem *>(a.plan + plan_items_at(s));
-  PlanJoin *joins = reinterpret_cast<PlanJoin *>(a.plan + plan_joins_at(s));
-  const int total = row0[s.n_seqs];
-  const int n_free = h->pad[0];
-  for (int64_t r = me; r < s.n_tokens; r += all) {
+  for (int r = me; r < s.n_tokens; r += all) {
     int pos = 0, slot = -1;
     if (r < total) {
-      const int q = last_at_or_before(row0, s.n_seqs, (int)r);
+      const int q = last_at_or_before(row0, s.n_seqs, r);
       const PlanSeq sq = seqs[q];
-      pos = sq.cached + (int)r - sq.row0;
-      const int idx = pos / s.page_size, off = pos % s.page_size;
+      pos = sq.cached + r - sq.row0;
+      const int idx = pos >> a.page_shift, off = pos & ((1 << a.page_shift) - 1);
       if (idx < s.max_pages) {
         int32_t *entry = a.table + (int64_t)q * s.max_pages + idx;
         int page;
         if (idx >= sq.has) {                                 // a new page, whose first position is a row of this step
-          const int rank = sq.page0 + idx - sq.has;
+          const int rank = add_capped(sq.page0, idx - sq.has);
           page = rank < n_free ? a.free_pages[n_free - 1 - rank] : -1;
           if (off == 0) *entry = page;
         } else {
           page = *entry;
         }
-        if ((uint32_t)page < (uint32_t)s.n_pages) slot = page * s.page_size + off;
+        if ((uint32_t)page < (uint32_t)s.n_pages) slot = (page << a.page_shift) + off;
       }
     }
     a.pos[r] = pos;
     a.slot[r] = slot;
   }
-  const int G = s.n_q_heads / s.n_kv_heads, bt = plan_block_tokens(s), jt = plan_join_tokens(s);
-  const int64_t cap = (int64_t)s.max_pages * s.page_size;
-  for (int64_t i = me; i < h->n_items; i += all) {
-    const int q = last_at_or_before(item0, s.n_seqs, (int)i);
+  const int bt = a.block.d, jt = a.join.d, cap = s.max_pages << a.page_shift;
+  for (int i = me; i < n_items; i += all) {
+    const int q = last_at_or_before(item0, s.n_seqs, i);
     const PlanSeq sq = seqs[q];
-    const int local = (int)i - sq.item0, n_blocks = (sq.rows + bt - 1) / bt;
-    const int b = n_blocks - 1 - local / sq.n_parts, j = local % sq.n_parts;    // the last block, which has most keys, first
+    const int local = i - sq.item0, n_blocks = a.block(sq.rows + bt - 1);
+    const int nth = sq.n_parts == 1 ? local : local / sq.n_parts, j = local - nth * sq.n_parts;
+    const int b = n_blocks - 1 - nth;                        // the last block, which has most keys, first
     const int n_tok = sq.rows - b * bt < bt ? sq.rows - b * bt : bt, p0 = sq.cached + b * bt;
-    const int64_t end = (int64_t)p0 + n_tok < cap ? p0 + n_tok : cap;
+    const int end = p0 + n_tok < cap ? p0 + n_tok : cap;
     const int lo = s.window > 0 && p0 >= s.window ? (p0 - s.window + 1) / kPlanTile : 0;
-    const int hi = (int)((end + kPlanTile - 1) / kPlanTile), n = hi > lo ? hi - lo : 0;
+    const int hi = (end + kPlanTile - 1) / kPlanTile, n = hi > lo ? hi - lo : 0;
     PlanItem it;
     it.seq = q;
     it.row0 = sq.row0 + b * bt;
     it.n_tok = n_tok;
     it.pos0 = p0;
-    it.tile0 = lo + (int)((int64_t)n * j / sq.n_parts);
-    it.tile1 = lo + (int)((int64_t)n * (j + 1) / sq.n_parts);
     it.part0 = -1;
     it.pad = 0;
     if (sq.n_parts > 1) {
-      const int first = sq.part0 + b * sq.n_parts * bt * G;
-      it.part0 = first + j * n_tok * G;
+      // n = each * parts + more: the first `more` parts get one tile more
+      const int each = n / sq.n_parts, more = n - each * sq.n_parts, first = sq.part0 + b * sq.n_parts * bt * a.G;
+      it.tile0 = lo + j * each + (j < more ? j : more);
+      it.tile1 = it.tile0 + each + (j < more ? 1 : 0);
+      it.part0 = first + j * n_tok * a.G;
       if (j == 0)
         for (int e = 0, t = 0; t < n_tok; ++e, t += jt)
-          joins[sq.join0 + b * (bt / jt) + e] = {it.row0 + t, n_tok - t < jt ? n_tok - t : jt, first + t * G, sq.n_parts, n_tok * G, {0, 0, 0}};
+          a.joins[sq.join0 + b * a.join(bt) + e] = {it.row0 + t, n_tok - t < jt ? n_tok - t : jt, first + t * a.G, sq.n_parts, n_tok * a.G, {0, 0, 0}};
+    } else {
+      it.tile0 = lo;
+      it.tile1 = lo + n;
     }
-    items[i] = it;
+    a.items[i] = it;
   }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(const PlanArgs a) {
-  __shared__ Sums scan[kPlanThreads / 64];
-  __shared__ int32_t row0[PRISM_MAX_CANDS + 1], item0[PRISM_MAX_CANDS];
-  constexpr int kPer = PRISM_MAX_CANDS / kPlanThreads;
+// THREADS threads take the sums of up to PER * THREADS sequences
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
+  constexpr bool kRecords = THREADS * PER <= kPlanInLds;     // the sequences' records in LDS too, for laying rows out
+  __shared__ Sums scan[THREADS / 64];
+  __shared__ int64_t tile_sums[THREADS / 64];
+  __shared__ int32_t row0[kRecords ? THREADS * PER : 1], item0[kRecords ? THREADS * PER : 1];
+  __shared__ PlanSeq records[kRecords ? THREADS * PER : 1];
   const prism_page_shape &s = a.s;
-  const int per = (s.n_seqs + kPlanThreads - 1) / kPlanThreads, first = threadIdx.x * per;
-  const int bt = plan_block_tokens(s), jt = plan_join_tokens(s), G = s.n_q_heads / s.n_kv_heads;
-  const int64_t cap = (int64_t)s.max_pages * s.page_size;
-  PlanHeader *h = reinterpret_cast<PlanHeader *>(a.plan);
-  PlanSeq *seqs = reinterpret_cast<PlanSeq *>(a.plan + sizeof(PlanHeader));
+  const int first = threadIdx.x * PER, bt = a.block.d, jt = a.join.d, psize = 1 << a.page_shift, cap = s.max_pages << a.page_shift;
 
   int n_free = *a.n_free;
   n_free = n_free < 0 ? 0 : n_free > a.free_cap ? a.free_cap : n_free;
-  int cached[kPer], rows[kPer], tiles[kPer];
+  int cached[PER], rows[PER], tiles[PER], has[PER], fresh_pages[PER], n_blocks[PER], n_parts[PER], r0[PER];
   Sums total, mine = {0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const bool in = k < per && first + k < s.n_seqs;
+  for (int k = 0; k < PER; ++k) {
+    const bool in = first + k < s.n_seqs;
     const int c = in ? a.cached[first + k] : 0, f = in ? a.fresh[first + k] : 0;
     cached[k] = c < 0 ? 0 : c > (1 << 29) ? 1 << 29 : c;
-    rows[k] = f < 0 ? 0 : f > s.n_tokens ? s.n_tokens : f;   // the sums stay far below 2^63
-    mine.a += rows[k];
+    rows[k] = f < 0 ? 0 : f;
+    mine.a = add_capped(mine.a, rows[k]);
   }
-  int64_t at = block_scan(mine, scan, total).a - mine.a;
-  const int64_t asked = total.a;
+  Sums run = block_scan<THREADS / 64>(mine, scan, total);
+  const int asked = total.a, done = asked < s.n_tokens ? asked : s.n_tokens;
   // rows behind the last of T are left out; pages, blocks and tiles of what is left
-  int64_t r0[kPer], blocks_tiles = 0;
-  int has[kPer], fresh_pages[kPer], n_blocks[kPer];
+  int at = run.a;
+  int64_t block_tiles = 0;
   mine = {0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     r0[k] = at < s.n_tokens ? at : s.n_tokens;
-    at += rows[k];
-    rows[k] = (int)((at < s.n_tokens ? at : s.n_tokens) - r0[k]);
-    const int64_t end = (int64_t)cached[k] + rows[k];
-    const int64_t hp = ((int64_t)cached[k] + s.page_size - 1) / s.page_size, np = (end + s.page_size - 1) / s.page_size;
-    has[k] = (int)(hp < s.max_pages ? hp : s.max_pages);
-    fresh_pages[k] = rows[k] > 0 ? (int)(np < s.max_pages ? np : s.max_pages) - has[k] : 0;
-    n_blocks[k] = (rows[k] + bt - 1) / bt;
-    int64_t t = ((end < cap ? end : cap) + kPlanTile - 1) / kPlanTile;
+    at = add_capped(at, rows[k]);
+    rows[k] = (at < s.n_tokens ? at : s.n_tokens) - r0[k];
+    const int end = cached[k] + rows[k];                     // below 2^30
+    const int hp = (cached[k] + psize - 1) >> a.page_shift, np = (end + psize - 1) >> a.page_shift;
+    has[k] = hp < s.max_pages ? hp : s.max_pages;
+    fresh_pages[k] = rows[k] > 0 ? (np < s.max_pages ? np : s.max_pages) - has[k] : 0;
+    n_blocks[k] = a.block(rows[k] + bt - 1);
+    int t = ((end < cap ? end : cap) + kPlanTile - 1) / kPlanTile;
     if (s.window > 0) {                                      // tiles that a block's window can touch
-      const int64_t w = ((int64_t)s.window + bt - 1 + kPlanTile - 1) / kPlanTile + 1;
+      const int w = (int)(((int64_t)s.window + bt + kPlanTile - 2) / kPlanTile) + 1;
       t = t < w ? t : w;
     }
-    tiles[k] = (int)t;
-    blocks_tiles += t * n_blocks[k];
-    mine.a += fresh_pages[k];
+    tiles[k] = t;
+    block_tiles += (int64_t)t * n_blocks[k];
+    mine.a = add_capped(mine.a, fresh_pages[k]);
   }
-  mine.b = blocks_tiles;
-  Sums run = block_scan(mine, scan, total);
-  int64_t page = run.a - mine.a;
-  const int64_t pages = total.a;
-  const int64_t goal = plan_goal(s);
-  int64_t per_item = (total.b + goal - 1) / goal;
-  if (per_item < kPlanMinTiles) per_item = kPlanMinTiles;
-  int n_parts[kPer];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) block_tiles += __shfl_xor(block_tiles, o, 64);
+  if ((threadIdx.x & 63) == 0) tile_sums[threadIdx.x >> 6] = block_tiles;
+  run = block_scan<THREADS / 64>(mine, scan, total);
+  int page = run.a;
+  const int pages = total.a;
+  int64_t all_tiles = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) all_tiles += tile_sums[w];
+  // Tiles of an item, rounded up, so at least the quotient (exact below 2^53): what bounds the number of items
+  auto share = [&](int goal, int least) {
+    const double x = ceil((double)all_tiles / goal);
+    return x < least ? least : x > 1 << 30 ? 1 << 30 : (int)x;
+  };
+  const int narrow = share(a.goal, kPlanMinTiles), wide = share(a.wide_goal, kPlanMinWide);
   mine = {0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    n_parts[k] = (int)((tiles[k] + per_item - 1) / per_item);
-    if (n_parts[k] < 1) n_parts[k] = 1;
-    mine.a += (int64_t)n_blocks[k] * n_parts[k];
+  for (int k = 0; k < PER; ++k) {
+    const bool one = rows[k] * a.G <= kPlanNarrow;
+    const int per_item = one ? narrow : wide;
+    n_parts[k] = (one ? tiles[k] > narrow : tiles[k] > wide + wide / 2) ? (tiles[k] + per_item - 1) / per_item : 1;
+    mine.a += n_blocks[k] * n_parts[k];
     if (n_parts[k] > 1) {
-      mine.b += (int64_t)rows[k] * G * n_parts[k];
-      mine.c += (rows[k] + jt - 1) / jt;
+      mine.b += rows[k] * a.G * n_parts[k];
+      mine.c += a.join(rows[k] + jt - 1);
     }
   }
-  run = block_scan(mine, scan, total);
-  int64_t item = run.a - mine.a, part = run.b - mine.b, join = run.c - mine.c;
+  run = block_scan<THREADS / 64>(mine, scan, total);
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     const int q = first + k;
-    if (k >= per || q >= s.n_seqs) continue;
-    PlanSeq o;
-    o.row0 = (int)r0[k];
-    o.rows = rows[k];
-    o.cached = cached[k];
-    o.has = has[k];
-    o.page0 = (int)(page < n_free ? page : n_free);          // ranks from n_free on have no page, however many there are
-    o.n_parts = n_parts[k];
-    o.item0 = (int)item;
-    o.part0 = (int)part;
-    o.join0 = (int)join;
-    o.pad[0] = o.pad[1] = o.pad[2] = 0;
-    seqs[q] = o;
-    row0[q] = o.row0;
-    item0[q] = o.item0;
+    if (q >= s.n_seqs) break;
+    const PlanSeq o = {r0[k], rows[k], cached[k], has[k], page, n_parts[k], run.a, run.b, run.c, {0, 0, 0}};
+    a.seqs[q] = o;
+    if (kRecords) {
+      row0[q] = o.row0;
+      item0[q] = o.item0;
+      records[q] = o;
+    }
     a.cu[q] = o.row0;
-    page += fresh_pages[k];
-    item += (int64_t)n_blocks[k] * n_parts[k];
+    page = add_capped(page, fresh_pages[k]);
+    run.a += n_blocks[k] * n_parts[k];
     if (n_parts[k] > 1) {
-      part += (int64_t)rows[k] * G * n_parts[k];
-      join += (rows[k] + jt - 1) / jt;
+      run.b += rows[k] * a.G * n_parts[k];
+      run.c += a.join(rows[k] + jt - 1);
     }
   }
   if (threadIdx.x == 0) {
-    const int64_t done = asked < s.n_tokens ? asked : s.n_tokens, taken = pages < n_free ? pages : n_free;
-    row0[s.n_seqs] = a.cu[s.n_seqs] = (int)done;
-    *a.n_free_left = (int)(n_free - taken);
+    const int taken = pages < n_free ? pages : n_free;
+    a.cu[s.n_seqs] = done;
+    *a.n_free_left = n_free - taken;
     if (a.status) {
-      const int64_t most = INT32_MAX;
-      a.status[0] = (int)done;
-      a.status[1] = (int)taken;
-      a.status[2] = (int)(pages - taken < most ? pages - taken : most);
-      a.status[3] = (int)(asked - done < most ? asked - done : most);
+      a.status[0] = done;
+      a.status[1] = taken;
+      a.status[2] = pages - taken;
+      a.status[3] = asked - done;
     }
     PlanHeader o;
     o.magic = kPlanMagic;
     o.shape = s;
-    o.n_items = (int)total.a;
-    o.n_joins = (int)total.c;
-    o.pad[0] = n_free;                                       // the caller's count may be overwritten before the rows are laid out
-    for (int k = 1; k < 5; ++k) o.pad[k] = 0;
-    *h = o;
+    o.n_items = total.a;
+    o.n_joins = total.c;
+    o.n_free = n_free;                                       // the caller's count may be overwritten before the rows are laid out
+    for (int k = 0; k < 4; ++k) o.pad[k] = 0;
+    *a.head = o;
   }
-  if (s.n_tokens > kPlanAlone) return;
+  if (!kRecords || s.n_tokens > kPlanAlone) return;
   __syncthreads();
-  lay_out(a, row0, item0, threadIdx.x, kPlanThreads);
+  lay_out(a, row0, item0, records, done, total.a, n_free, threadIdx.x, THREADS);
 }
 
 __global__ __launch_bounds__(256) void page_rows_kernel(const PlanArgs a) {
-  __shared__ int32_t row0[PRISM_MAX_CANDS + 1], item0[PRISM_MAX_CANDS];
-  const PlanSeq *seqs = reinterpret_cast<const PlanSeq *>(a.plan + sizeof(PlanHeader));
+  __shared__ int32_t row0[PRISM_MAX_CANDS], item0[PRISM_MAX_CANDS];
   for (int i = threadIdx.x; i < a.s.n_seqs; i += 256) {
-    row0[i] = seqs[i].row0;
-    item0[i] = seqs[i].item0;
+    row0[i] = a.seqs[i].row0;
+    item0[i] = a.seqs[i].item0;
   }
-  if (threadIdx.x == 0) row0[a.s.n_seqs] = a.cu[a.s.n_seqs];
+  const int total = a.cu[a.s.n_seqs], n_items = a.head->n_items, n_free = a.head->n_free;
   __syncthreads();
-  lay_out(a, row0, item0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+  lay_out(a, row0, item0, a.seqs, total, n_items, n_free, (int)(blockIdx.x * 256 + threadIdx.x), (int)(gridDim.x * 256));
 }
 
 int check_page_shape(const prism_page_shape *s, const char *who) {
@@ -282,11 +295,28 @@ extern "C" int prism_op_page_plan(const prism_page_shape *shape, const int32_t *
   PRISM_REQUIRE(shape->n_seqs == 0 || (cached && fresh && table), PRISM_EINVAL, "page_plan: bad arguments");
   PRISM_REQUIRE(shape->n_tokens == 0 || (pos && slot), PRISM_EINVAL, "page_plan: bad arguments");
   PRISM_REQUIRE((uintptr_t)plan % 16 == 0, PRISM_EINVAL, "page_plan: the plan must be 16-byte aligned");
-  PlanArgs a = {*shape, cached, fresh, table, free_pages, n_free, free_cap, n_free_left, cu, pos, slot, status, (char *)plan};
+  PlanArgs a;
+  a.s = *shape;
+  a.cached = cached; a.fresh = fresh; a.table = table; a.free_pages = free_pages; a.n_free = n_free;
+  a.n_free_left = n_free_left; a.cu = cu; a.pos = pos; a.slot = slot; a.status = status;
+  a.head = (PlanHeader *)plan;
+  a.seqs = (PlanSeq *)((char *)plan + sizeof(PlanHeader));
+  a.items = (PlanItem *)((char *)plan + plan_items_at(*shape));
+  a.joins = (PlanJoin *)((char *)plan + plan_joins_at(*shape));
+  a.block = divisor(plan_block_tokens(*shape));
+  a.join = divisor(plan_join_tokens(*shape));
+  a.free_cap = free_cap;
+  a.page_shift = __builtin_ctz(shape->page_size);
+  a.G = shape->n_q_heads / shape->n_kv_heads;
+  a.goal = plan_goal(*shape);
+  a.wide_goal = plan_wide_goal(*shape);
   hipStream_t s = (hipStream_t)stream;
-  page_plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
+  // few sequences and rows: as many waves as have something to do, since every barrier waits for all of them
+  if (shape->n_seqs <= 256 && shape->n_tokens <= 1024) page_plan_kernel<256, 1><<<1, 256, 0, s>>>(a);
+  else if (shape->n_seqs <= kPlanInLds) page_plan_kernel<1024, 1><<<1, 1024, 0, s>>>(a);
+  else page_plan_kernel<1024, PRISM_MAX_CANDS / 1024><<<1, 1024, 0, s>>>(a);
   PRISM_HIP(hipGetLastError());
-  if (shape->n_tokens > kPlanAlone) {
+  if (shape->n_tokens > (shape->n_seqs > kPlanInLds ? 0 : kPlanAlone)) {
     const int grid = cdiv(shape->n_tokens, 512);
     page_rows_kernel<<<grid < 1024 ? grid : 1024, 256, 0, s>>>(a);
     PRISM_HIP(hipGetLastError());

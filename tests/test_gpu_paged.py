@@ -36,14 +36,14 @@ def _check_work(plan, cu, cached, page, width, G, nkv, window):
     raw = plan.buffer.cpu().numpy().view(np.int32)
     n_items, n_joins = int(raw[9]), int(raw[10])
     n = plan.n_seqs
-    goal, jt = -(-1024 // nkv), max(1, 16 // G)
+    goal, jt = -(-1024 // nkv), max(1, 8 // G)
     bt = 128 // G // jt * jt
     items_at = 16 + 12 * n
     most = plan.n_tokens // bt + n + goal
     assert n_items <= most
     items = raw[items_at: items_at + 8 * n_items].reshape(-1, 8)
     joins = raw[items_at + 8 * most:][: 8 * n_joins].reshape(-1, 8)
-    room = min(2 * goal * 128, plan.n_tokens * G * (goal + 1))
+    room = min(goal * 128, plan.n_tokens * G * (goal + 1))
     seen, parts = {}, {}
     for seq, row0, n_tok, pos0, t0, t1, part, _ in items.tolist():
         assert 0 <= seq < n and 1 <= n_tok <= bt and cu[seq] <= row0 and row0 + n_tok <= cu[seq + 1] and (row0 - cu[seq]) % bt == 0
