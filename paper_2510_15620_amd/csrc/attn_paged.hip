@@ -70,6 +70,16 @@ template <typename V8> __device__ __forceinline__ V8 join_halves(s16x4 a, s16x4 
   return u.v;
 }
 
+// A value that nothing writes while the kernel runs, at an address that is the same for the whole wave: by the scalar unit, so that
+// waiting for it is not waiting for the loads of K and V that are under way
+template <typename T> __device__ __forceinline__ T load_const(const T *p) {
+  typedef const __attribute__((address_space(4))) uint32_t *Words;
+  union { T v; uint32_t w[sizeof(T) / 4]; } u;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) u.w[i] = ((Words)(uintptr_t)p)[i];
+  return u.v;
+}
+
 // Until at most N of this wave's memory accesses are under way.  They end in their order; others among them only make it wait longer
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -121,8 +131,9 @@ void attention_paged_16_kernel(const PagedAttn a) {
 
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
-  const PlanItem it = a.items[item];                          // within the list's room, whatever it holds: asked for with the header
-  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || item >= a.plan->n_items) return;
+  const PlanItem it = load_const(a.items + item);             // within the list's room, whatever it holds: asked for with the header
+  const PlanHeader plan = load_const(a.plan);
+  if (plan.magic != kPlanMagic || !same_shape(plan.shape, a.shape) || item >= plan.n_items) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = it.n_tok * G, window = a.shape.window;
   const int cap_keys = a.shape.max_pages << a.page_shift;
@@ -137,7 +148,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
   // page of the 16 keys from k0 (a multiple of 16) on; none: -1
   auto page_of = [&](int k0) __attribute__((always_inline)) {
     if (k0 >= limit) return -1;
-    const int p = table[k0 >> a.page_shift];
+    const int p = load_const(table + (k0 >> a.page_shift));
     return (unsigned)p < (unsigned)a.shape.n_pages ? p : -1;
   };
   // values in front of those keys' rows; keys without a page read the first one, under the mask
@@ -273,8 +284,12 @@ void attention_paged_16_kernel(const PagedAttn a) {
               pf[b][kb * 4 + e + 1] = ph[1];
             }
           l_run[b] = l_run[b] * alpha + psum;
+          unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);   // as below
+          asm volatile("" : "+s"(moved));
+          if (moved != 0) {
 #pragma unroll
-          for (int t = 0; t < HD / 16; ++t) o[b][t] *= alpha;
+            for (int t = 0; t < HD / 16; ++t) o[b][t] *= alpha;
+          }
         }
         vec8 vf[HD / 16];
         if (more) wait_loads<2 * NI>();                      // V's have landed when only the next K's are under way
@@ -429,16 +444,35 @@ void attention_paged_16_kernel(const PagedAttn a) {
   const int vr = 4 * half + ((lane & 15) >> 2), vc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
   const int rdV = vr * HD + (vc ^ swizzle_v<HD>(vr)) * 8 + (lane & 1) * 4;                                 // t flips the bits from 4 on
 
-  // of the 64 keys from k0 on: some row of the wave may see some; some row sees a key that another does not, or some do not exist
+  // of the 64 keys from k0 on: some row of the wave may see some; some row of the wave sees a key that another does not, or some keys do
+  // not exist; the same for any two rows of the block
   auto touched = [&](int k0) __attribute__((always_inline)) { return active && k0 <= w_last && (window == 0 || k0 + 63 > w_first - window); };
-  auto mixed = [&](int k0) __attribute__((always_inline)) { return k0 + 63 > w_first || k0 + 63 >= limit || (window > 0 && k0 <= w_last - window); };
-  bool odd = false;                                           // values that are not finite were taken out of such a tile
+  auto mixed = [&](int k0, int first, int last) __attribute__((always_inline)) {
+    return k0 + 63 > first || k0 + 63 >= limit || (window > 0 && k0 <= last - window);
+  };
+  // A tile in which some rows of the block do not see some keys: a weight of zero times a value that is not finite would reach the sum.
+  // So before the others read it, a wave clears what it staged of keys that nobody sees, and of the other keys what is not finite; those
+  // values are added where they are seen, at the end (`odd`).
+  bool odd = false;
+  auto clean = [&](int kt, int page, auto buf_tag) __attribute__((always_inline)) {
+    OT *const v = (decltype(buf_tag)::value ? lV1 : lV0) + wave * 16 * HD + lane * 8;
+    wait_loads<0>();
+    u16x2 worst = {0, 0};
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const unsigned there = page >= 0 && kt * 64 + wave * 16 + j * RI + lane / CH < limit ? ~0u : 0u;
+      const u32x4 x = clean_fragment(*reinterpret_cast<const u32x4 *>(v + j * RI * HD), u32x4{there, there, there, there}, worst);
+      *reinterpret_cast<u32x4 *>(v + j * RI * HD) = finite_only<OT>(x);
+    }
+    odd = odd || __builtin_amdgcn_ballot_w64(not_finite<OT>(worst)) != 0;
+  };
   const int kt_end = it.tile1;
   Pages cur = {-1, 0}, next = {-1, 0}, after = {-1, 0};
   if (it.tile0 < kt_end) {
     cur = pages_of(it.tile0);
     stage(it.tile0, cur.own, std::integral_constant<int, 0>{});
     if (it.tile0 + 1 < kt_end) next = pages_of(it.tile0 + 1);
+    if (cur.there != 15u || mixed(it.tile0 * 64, it.pos0, last)) clean(it.tile0, cur.own, std::integral_constant<int, 0>{});
   }
   __syncthreads();                                            // also waits for this wave's own loads
 
@@ -451,38 +485,39 @@ void attention_paged_16_kernel(const PagedAttn a) {
       if (kt + 2 < kt_end) after = pages_of(kt + 2);
     }
     const int k0 = kt * 64, kh = k0 + 4 * half;
-    auto tile_step = [&](auto mask_tag) __attribute__((always_inline)) {
-      constexpr bool MASK = decltype(mask_tag)::value;
+    if (touched(k0)) {
       int atK = rdK, atV = rdV;                               // opaque: the 16 addresses of either stage are one instruction each to make,
       asm volatile("" : "+v"(atK), "+v"(atV));                // and registers that spill if they are kept over the loop
       f32x16 s[2];
       vec8 kf[2][HD / 16];
-      auto read_k = [&](int kb) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) kf[kb][kk] = *reinterpret_cast<const vec8 *>(&lK[(atK ^ (kk * 16)) + kb * 32 * HD]);
-      };
-      read_k(0);
-      if (!MASK) read_k(1);                                   // (the masked form has no registers to spare)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
         if (kb == 1) __builtin_amdgcn_sched_barrier(0);
-        if (MASK && kb == 1) read_k(1);
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) s[kb] = Mfma<OT>::mma(kf[kb][kk], qf[kk], s[kb]);
       }
-      if (MASK || MOD) {
-        const int lo = (window > 0 ? pos - window + 1 : 0) - kh, hi = (pos < limit - 1 ? pos : limit - 1) - kh, away = pos - kh;
+      // key kb * 32 + (e / 4) * 8 + e % 4 from kh on
+      if (MOD) {
+        const int away = pos - kh;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kb][e] = modified_score(s[kb][e], a.scale, a.softcap, inv_cap, slope, away - (kb * 32 + (e >> 2) * 8 + (e & 3)));
+      }
+      if (cur.there != 15u || mixed(k0, w_first, w_last)) {
+        const int lo = (window > 0 ? pos - window + 1 : 0) - kh, hi = (pos < limit - 1 ? pos : limit - 1) - kh;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int key = kb * 32 + (e >> 2) * 8 + (e & 3);   // from kh on
-            if (MOD) s[kb][e] = modified_score(s[kb][e], a.scale, a.softcap, inv_cap, slope, away - key);
-            if (MASK) {
-              if (!(key >= lo && key <= hi && (cur.there >> (kb * 2 + (e >> 3)) & 1))) s[kb][e] = -INFINITY;
-            }
+            const int key = kb * 32 + (e >> 2) * 8 + (e & 3);
+            if (!(key >= lo && key <= hi && (cur.there >> (kb * 2 + (e >> 3)) & 1))) s[kb][e] = -INFINITY;
           }
       }
       float mxk[2] = {-INFINITY, -INFINITY};
@@ -492,7 +527,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
         for (int e = 0; e < 16; ++e) mxk[kb] = fmaxf(mxk[kb], s[kb][e]);
       const float mx = max_xor32(fmaxf(mxk[0], mxk[1]));
       const float m_new = fmaxf(m_run, mx);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float ref = m_new == -INFINITY ? 0.f : m_new;     // no key yet: weights exp(-inf) = 0
       const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c_exp), mb = ref * c_exp - P16::kLift;
       float psum = 0.f;
       vec8 pf[4];
@@ -518,43 +553,17 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
       }
-      u32x4 keep[4];
-      if (MASK) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+      for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int key = ks * 16 + (w >> 1) * 8 + (w & 1) * 2;
-            const bool page = cur.there >> ks & 1;
-            keep[ks][w] = (page && key < limit - kh ? 0xFFFFu : 0u) | (page && key + 1 < limit - kh ? 0xFFFF0000u : 0u);
-          }
-      }
-#pragma unroll
-      for (int t = 0; t < HD / 32; ++t) {
-        vec8 vf[4];
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          vf[ks] = join_halves<vec8>(read_transposed(&lV[(atV ^ (t * 32)) + ks * 16 * HD]), read_transposed(&lV[(atV ^ (t * 32)) + (ks * 16 + 8) * HD]));
-        if (MASK) {
-          u16x2 worst = {0, 0};
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) vf[ks] = __builtin_bit_cast(vec8, clean_fragment(__builtin_bit_cast(u32x4, vf[ks]), keep[ks], worst));
-          if (__builtin_amdgcn_ballot_w64(not_finite<OT>(worst)) != 0) {
-            odd = true;
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) vf[ks] = __builtin_bit_cast(vec8, finite_only<OT>(__builtin_bit_cast(u32x4, vf[ks])));
-          }
+        for (int ks = 0; ks < 4; ++ks) {
+          const vec8 vf = join_halves<vec8>(read_transposed(&lV[(atV ^ (t * 32)) + ks * 16 * HD]), read_transposed(&lV[(atV ^ (t * 32)) + (ks * 16 + 8) * HD]));
+          o[t] = Mfma<OT>::mma(vf, pf[ks], o[t]);
         }
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) o[t] = Mfma<OT>::mma(vf[ks], pf[ks], o[t]);
-      }
-    };
-    if (touched(k0)) {
-      if (cur.there != 15u || mixed(k0)) tile_step(std::true_type{});
-      else tile_step(std::false_type{});
     }
     cur = next;
     next = after;
+    if (kt + 1 < kt_end && (cur.there != 15u || mixed(k0 + 64, it.pos0, last))) clean(kt + 1, cur.own, std::integral_constant<int, CUR ^ 1>{});
     __syncthreads();                                          // the next tile has landed and everyone is done with this one
   };
   for (int kt = it.tile0; kt < kt_end; kt += 2) {
@@ -562,10 +571,17 @@ void attention_paged_16_kernel(const PagedAttn a) {
     if (kt + 1 < kt_end) step(kt + 1, std::integral_constant<int, 1>{});
   }
 
+  // any wave's clearing concerns all rows
+  int *const odd_waves = reinterpret_cast<int *>(lK0);
+  if (lane == 0) odd_waves[wave] = odd;
+  __syncthreads();
+  odd = odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3];
+  const float l_tot = sum_xor32(l_run);
+  if (!active || r_first + c >= rows) return;
   // lane holds d = 32 t + 8 (e / 4) + 4 half + e % 4 of its row
   if (odd) {
     for (int kt = it.tile0; kt < kt_end; ++kt) {
-      if (!touched(kt * 64) || !(mixed(kt * 64) || pages_of(kt).there != 15u)) continue;
+      if (pages_of(kt).there == 15u && !mixed(kt * 64, it.pos0, last)) continue;
       for (int k0 = kt * 64; k0 < kt * 64 + 64 && k0 < limit; k0 += 16) {
         const int page = page_of(k0);
         if (page < 0) continue;
@@ -584,8 +600,6 @@ void attention_paged_16_kernel(const PagedAttn a) {
       }
     }
   }
-  const float l_tot = sum_xor32(l_run);
-  if (!active || r_first + c >= rows) return;
   if (it.part0 < 0) {
     const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
     OT *op = (OT *)a.out + (int64_t)(it.row0 + tok) * a.out_stride + (int64_t)head * HD + half * 4;
