@@ -70,16 +70,6 @@ template <typename V8> __device__ __forceinline__ V8 join_halves(s16x4 a, s16x4 
   return u.v;
 }
 
-// A value that nothing writes while the kernel runs, at an address that is the same for the whole wave: by the scalar unit, so that
-// waiting for it is not waiting for the loads of K and V that are under way
-template <typename T> __device__ __forceinline__ T load_const(const T *p) {
-  typedef const __attribute__((address_space(4))) uint32_t *Words;
-  union { T v; uint32_t w[sizeof(T) / 4]; } u;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) u.w[i] = ((Words)(uintptr_t)p)[i];
-  return u.v;
-}
-
 // Until at most N of this wave's memory accesses are under way.  They end in their order; others among them only make it wait longer
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -107,14 +97,26 @@ template <typename OT> __device__ __forceinline__ float infinite_only(OT v) {
   return fabsf(x) < INFINITY ? 0.f : x;
 }
 
-// Scores in units of log 2: cap tanh(s scale / cap) - slope (p - k), all times log2(e).  1 - 2 / (1 + e^2u) is tanh(u) to some 1e-7,
-// absolute: less than the rounding of the scores' operands.
-__device__ __forceinline__ float modified_score(float s, float scale, float cap, float inv_cap, float slope, int away) {
-  constexpr float kLog2e = 1.4426950408889634f;
-  float x = s * scale;
-  if (cap > 0.f) x = cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * inv_cap * (2.0f * kLog2e))));
-  return (x - slope * (float)away) * kLog2e;
-}
+// Scores with a cap, slopes or both, in units of log 2: (cap tanh(s scale / cap) - slope (p - k)) log2(e).  With tanh(u) = 1 - 2 / (1 + e^2u),
+// good to some 1e-7 absolutely (less than the rounding of the scores' operands), a score is one of
+//   -2 cap / (1 + 2^(in s)) + (slope k + rest),   in s + (slope k + rest)
+// where the factors hold scale and log2(e), k counts from the tile's first key of the lane and rest has cap, slope and the row's position.
+struct Modifier {
+  float in, minus_two_cap, slope, rest;
+  bool capped;
+  __device__ __forceinline__ Modifier(float scale, float cap, float slope_, int away) {
+    constexpr float kLog2e = 1.4426950408889634f;
+    capped = cap > 0.f;
+    in = capped ? scale * (2.0f * kLog2e) / cap : scale * kLog2e;
+    minus_two_cap = -2.0f * cap * kLog2e;
+    slope = slope_ * kLog2e;
+    rest = (capped ? cap * kLog2e : 0.f) - slope * (float)away;
+  }
+  __device__ __forceinline__ float operator()(float s, int key) const {
+    const float bias = __builtin_fmaf(slope, (float)key, rest);
+    return capped ? __builtin_fmaf(minus_two_cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * in)), bias) : __builtin_fmaf(s, in, bias);
+  }
+};
 
 template <typename OT, int HD, bool MOD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -125,6 +127,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
   constexpr int CH = HD / 8;                                  // 16-byte chunks of a row
   constexpr int RI = 64 / CH;                                 // rows that a wave's load instruction moves
   constexpr int NI = 16 / RI;                                 // instructions for 16 rows
+  constexpr int VK = 2;                                     // groups of 16 keys whose V^T fragments are read ahead of the softmax
   // Four objects, so that the compiler knows which reads a load in flight cannot touch.  Wide: stages 0 and 1 of K and of V, 64 rows
   // each.  Narrow: 16 rows of each for every wave, keys 0-15 and 16-31 of its step.
   __shared__ __align__(16) OT lK0[64 * 128], lK1[64 * 128], lV0[64 * 128], lV1[64 * 128];
@@ -143,7 +146,6 @@ void attention_paged_16_kernel(const PagedAttn a) {
   const OT *const Kh = (const OT *)a.K + ((int64_t)kvh * HD << a.page_shift);
   const OT *const Vh = (const OT *)a.V + ((int64_t)kvh * HD << a.page_shift);
   const float c_exp = a.unit;                                 // scores times c_exp: in units of log 2
-  const float inv_cap = MOD && a.softcap > 0.f ? 1.0f / a.softcap : 0.f;
 
   // page of the 16 keys from k0 (a multiple of 16) on; none: -1
   auto page_of = [&](int k0) __attribute__((always_inline)) {
@@ -160,12 +162,18 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
   for (int j = 0; j < NI; ++j) {
     const int r = j * RI + lane / CH, c = lane % CH;
-    oK[j] = (r * HD + (c ^ swizzle_k<HD>(r)) * 8) * 2;       // bytes
-    oV[j] = (r * HD + (c ^ swizzle_v<HD>(r)) * 8) * 2;
+    oK[j] = (lane / CH * HD + (c ^ swizzle_k<HD>(r)) * 8) * 2;   // bytes, from the instruction's first row
+    oV[j] = (lane / CH * HD + (c ^ swizzle_v<HD>(r)) * 8) * 2;
   }
+  // 16 rows: an instruction's 1 KiB lies as far from the first one's in memory as in LDS, so the offset of both is an immediate
   auto load16 = [&](const OT *src, const uint32_t (&o)[NI], OT *dst) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < NI; ++j) __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(reinterpret_cast<const char *>(src) + o[j]), PRISM_LDS_PTR(dst + j * RI * HD), 16, 0, 0);
+    const char *const s = reinterpret_cast<const char *>(src);
+    __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[0]), PRISM_LDS_PTR(dst), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[1]), PRISM_LDS_PTR(dst), 16, 1024, 0);
+    if constexpr (NI == 4) {
+      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[2]), PRISM_LDS_PTR(dst), 16, 2048, 0);
+      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[3]), PRISM_LDS_PTR(dst), 16, 3072, 0);
+    }
   };
 
   if (rows <= 32) {
@@ -248,11 +256,11 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
           if (MOD) {
+            const Modifier modified(a.scale, a.softcap, slope[b], pos[b] - kg);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                s[b][kb][e] = modified_score(s[b][kb][e], a.scale, a.softcap, inv_cap, slope[b], pos[b] - kg - (kb * 16 + e));
+              for (int e = 0; e < 4; ++e) s[b][kb][e] = modified(s[b][kb][e], kb * 16 + e);
           }
           if (masked) {
             const int lo = (window > 0 ? pos[b] - window + 1 : 0) - kg, hi = (pos[b] < limit - 1 ? pos[b] : limit - 1) - kg;
@@ -494,6 +502,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) kf[kb][kk] = *reinterpret_cast<const vec8 *>(&lK[(atK ^ (kk * 16)) + kb * 32 * HD]);
+      __builtin_amdgcn_sched_barrier(0);                      // all under way before the first is waited for
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -502,13 +511,21 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) s[kb] = Mfma<OT>::mma(kf[kb][kk], qf[kk], s[kb]);
       }
+      vec8 vf[VK][HD / 32];
+      auto read_v = [&](int t, int ks) __attribute__((always_inline)) {
+        return join_halves<vec8>(read_transposed(&lV[(atV ^ (t * 32)) + ks * 16 * HD]), read_transposed(&lV[(atV ^ (t * 32)) + (ks * 16 + 8) * HD]));
+      };
+#pragma unroll
+      for (int ks = 0; ks < VK; ++ks)
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t) vf[ks][t] = read_v(t, ks);
       // key kb * 32 + (e / 4) * 8 + e % 4 from kh on
       if (MOD) {
-        const int away = pos - kh;
+        const Modifier modified(a.scale, a.softcap, slope, pos - kh);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[kb][e] = modified_score(s[kb][e], a.scale, a.softcap, inv_cap, slope, away - (kb * 32 + (e >> 2) * 8 + (e & 3)));
+          for (int e = 0; e < 16; ++e) s[kb][e] = modified(s[kb][e], kb * 32 + (e >> 2) * 8 + (e & 3));
       }
       if (cur.there != 15u || mixed(k0, w_first, w_last)) {
         const int lo = (window > 0 ? pos - window + 1 : 0) - kh, hi = (pos < limit - 1 ? pos : limit - 1) - kh;
@@ -525,6 +542,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mxk[kb] = fmaxf(mxk[kb], s[kb][e]);
+      __builtin_amdgcn_sched_barrier(0);
       const float mx = max_xor32(fmaxf(mxk[0], mxk[1]));
       const float m_new = fmaxf(m_run, mx);
       const float ref = m_new == -INFINITY ? 0.f : m_new;     // no key yet: weights exp(-inf) = 0
@@ -554,12 +572,13 @@ void attention_paged_16_kernel(const PagedAttn a) {
           for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
       }
 #pragma unroll
-      for (int t = 0; t < HD / 32; ++t)
+      for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          const vec8 vf = join_halves<vec8>(read_transposed(&lV[(atV ^ (t * 32)) + ks * 16 * HD]), read_transposed(&lV[(atV ^ (t * 32)) + (ks * 16 + 8) * HD]));
-          o[t] = Mfma<OT>::mma(vf, pf[ks], o[t]);
+        for (int t = 0; t < HD / 32; ++t) {
+          const vec8 v = ks < VK ? vf[ks < VK ? ks : 0][t] : read_v(t, ks);
+          o[t] = Mfma<OT>::mma(v, pf[ks], o[t]);
         }
+      }
     }
     cur = next;
     next = after;

@@ -19,8 +19,9 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   __shared__ float2 lml[4][16];
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
-  const PlanItem it = a.items[item];
-  if (a.plan->magic != kPlanMagic || !same_shape(a.plan->shape, a.shape) || item >= a.plan->n_items) return;
+  const PlanItem it = load_const(a.items + item);
+  const PlanHeader plan = load_const(a.plan);
+  if (plan.magic != kPlanMagic || !same_shape(plan.shape, a.shape) || item >= plan.n_items) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int rows = it.n_tok * G, row_begin = blockIdx.y * 64, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
   const int last = it.pos0 + it.n_tok - 1, limit = last + 1 < cap_keys ? last + 1 : cap_keys;
@@ -28,7 +29,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   const float *const Kh = (const float *)a.K + ((int64_t)kvh * HD << a.page_shift), *const Vh = (const float *)a.V + ((int64_t)kvh * HD << a.page_shift);
   auto page_of = [&](int k0) __attribute__((always_inline)) {
     if (k0 >= limit) return -1;
-    const int p = table[k0 >> a.page_shift];
+    const int p = load_const(table + (k0 >> a.page_shift));
     return (unsigned)p < (unsigned)a.shape.n_pages ? p : -1;
   };
   struct Tile { f32x4 k[NB]; float v[4][NB]; int page; };

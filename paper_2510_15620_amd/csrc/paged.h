@@ -77,6 +77,16 @@ int check_kv_cache(const prism_kv_cache *c, const char *who);
 template <typename T> __device__ __forceinline__ T round_to(float v) { return from_f32<T>(v); }
 template <> __device__ __forceinline__ f16 round_to<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }
 
+// A value that nothing writes while the kernel runs, at an address that is the same for the whole wave: by the scalar unit, so that
+// waiting for it is not waiting for the loads of K and V that are under way
+template <typename T> __device__ __forceinline__ T load_const(const T *p) {
+  typedef const __attribute__((address_space(4))) uint32_t *Words;
+  union { T v; uint32_t w[sizeof(T) / 4]; } u;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) u.w[i] = ((Words)(uintptr_t)p)[i];
+  return u.v;
+}
+
 // What an attention launch reads and writes.  Partial results of part row i and KV head h: values at O[(i * n_kv + h) * hd], running
 // maximum and sum of weights at ml[i * n_kv + h].  unit: from a difference of the maxima to the exponent of 2 that its weight has.
 struct PagedAttn {
