@@ -42,16 +42,6 @@ template <> struct Paged16<f16> {
   static __device__ __forceinline__ f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// max of v over lanes l, l ^ 16 / l, l ^ 32
-__device__ __forceinline__ float max_xor32(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float max_xor16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
 // Which 16-byte chunk of a row stands where in LDS (chunk c of row r at slot c ^ swizzle).  K: the 16 rows that one pass of a read
 // touches spread over all banks.  V: a transposing read takes 32 bytes of four rows per 16 lanes; the rows of one pass, four
 // consecutive keys and 64 bytes (wide items) or eight and 32 bytes (narrow), spread over all banks.
@@ -63,15 +53,32 @@ template <int HD> __device__ __forceinline__ constexpr int swizzle_v(int r) {
 template <typename OT> __device__ __forceinline__ s16x4 read_transposed(const OT *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
+// Reads whose results are waited for inside, for the loop that keeps loads to other places of LDS under way: in front of reads of its
+// own the compiler waits for all of them.
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)PRISM_LDS_PTR(p); }
+template <typename V8> __device__ __forceinline__ void read_rows(V8 (&r)[4], const uint32_t (&p)[4]) {
+  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]) : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]) : "memory");
+}
+template <typename V8> __device__ __forceinline__ void read_rows(V8 (&r)[8], const uint32_t (&p)[8]) {
+  asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+               "ds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\tds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+               : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]) : "memory");
+}
+__device__ __forceinline__ void read_transposed(s16x4 (&r)[8], const uint32_t (&p)[8]) {
+  asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %10\n\tds_read_b64_tr_b16 %3, %11\n\t"
+               "ds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\tds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\t"
+               "s_waitcnt lgkmcnt(0)"
+               : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+               : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]) : "memory");
+}
 template <typename V8> __device__ __forceinline__ V8 join_halves(s16x4 a, s16x4 b) {
   union { s16x4 h[2]; V8 v; } u;
   u.h[0] = a;
   u.h[1] = b;
   return u.v;
 }
-
-// Until at most N of this wave's memory accesses are under way.  They end in their order; others among them only make it wait longer
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // A V^T fragment of a tile in which some rows do not see some keys.  A weight of zero times a value that is not finite would reach the
 // sum, so: values of keys that no row sees (`keep` has their bits clear) become zero; `worst` collects the largest magnitude bits.
@@ -119,7 +126,7 @@ struct Modifier {
 };
 
 template <typename OT, int HD, bool MOD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 2 : 3, HD == 128 ? 2 : 3)))
 void attention_paged_16_kernel(const PagedAttn a) {
   typedef typename Mfma<OT>::vec8 vec8;
   typedef typename Mfma<OT>::vec4 vec4;
@@ -129,8 +136,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
   constexpr int NI = 16 / RI;                                 // instructions for 16 rows
   constexpr int VK = 2;                                     // groups of 16 keys whose V^T fragments are read ahead of the softmax
   // Four objects, so that the compiler knows which reads a load in flight cannot touch.  Wide: stages 0 and 1 of K and of V, 64 rows
-  // each.  Narrow: 16 rows of each for every wave, keys 0-15 and 16-31 of its step.
-  __shared__ __align__(16) OT lK0[64 * 128], lK1[64 * 128], lV0[64 * 128], lV1[64 * 128];
+  // each.  Narrow: 16 rows of each for every wave, keys 0-15 and 16-31 of its step.  Aligned so that flipping bits within a row is flipping them in the address.
+  __shared__ __align__(1024) OT lK0[64 * HD], lK1[64 * HD], lV0[64 * HD], lV1[64 * HD];
 
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
@@ -147,12 +154,11 @@ void attention_paged_16_kernel(const PagedAttn a) {
   const OT *const Vh = (const OT *)a.V + ((int64_t)kvh * HD << a.page_shift);
   const float c_exp = a.unit;                                 // scores times c_exp: in units of log 2
 
-  // page of the 16 keys from k0 (a multiple of 16) on; none: -1
-  auto page_of = [&](int k0) __attribute__((always_inline)) {
-    if (k0 >= limit) return -1;
-    const int p = load_const(table + (k0 >> a.page_shift));
-    return (unsigned)p < (unsigned)a.shape.n_pages ? p : -1;
-  };
+  // Table entry of the 16 keys from k0 on (a multiple of 16; behind the last key, that key's), and the page that it gives, none: -1.
+  // Apart, because waiting for a scalar load is waiting for all LDS reads under way: entries are asked for a step before they are used
+  auto entry_of = [&](int k0) __attribute__((always_inline)) { return load_const(table + ((k0 < limit ? k0 : limit - 1) >> a.page_shift)); };
+  auto page_from = [&](int entry, int k0) __attribute__((always_inline)) { return k0 < limit && (unsigned)entry < (unsigned)a.shape.n_pages ? entry : -1; };
+  auto page_of = [&](int k0) __attribute__((always_inline)) { return page_from(entry_of(k0), k0); };
   // values in front of those keys' rows; keys without a page read the first one, under the mask
   auto rows_at = [&](int page, int k0) __attribute__((always_inline)) {
     return (int64_t)(page < 0 ? 0 : page) * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
@@ -186,6 +192,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
     const int rdK = c * HD + ((g ^ (swizzle_k<HD>(c) & 3)) | (swizzle_k<HD>(c) & ~3)) * 8;      // kk flips the bits from 4 on
     const int vr = 4 * g + (c >> 2);
     const int rdV = vr * HD + (((c & 3) >> 1) ^ swizzle_v<HD>(vr)) * 8 + (c & 1) * 4;          // t flips the bits from 2 on
+    const uint32_t at_k0 = lds_address(k0p + rdK), at_k1 = lds_address(k1p + rdK), at_v0 = lds_address(v0p + rdV), at_v1 = lds_address(v1p + rdV);
     auto narrow = [&](auto rb_tag) __attribute__((always_inline)) {
       constexpr int RB = decltype(rb_tag)::value;            // blocks of 16 rows
       vec8 qf[RB][HD / 32];
@@ -211,125 +218,129 @@ void attention_paged_16_kernel(const PagedAttn a) {
       };
       bool odd = false;                                      // values that are not finite were taken out of such a step
       int st = it.tile0 * 2 + wave;
-      int pg0 = -1, pg1 = -1, nx0 = -1, nx1 = -1;            // pages of the step's two groups of 16 keys, and of the next step's
       if (st < s_end) {
-        pg0 = page_of(st * 32);
-        pg1 = page_of(st * 32 + 16);
+        int pg0 = page_of(st * 32), pg1 = page_of(st * 32 + 16);   // pages of the step's two groups of 16 keys
         load16(Kh + rows_at(pg0, st * 32), oK, k0p);
         load16(Kh + rows_at(pg1, st * 32 + 16), oK, k1p);
         load16(Vh + rows_at(pg0, st * 32), oV, v0p);
         load16(Vh + rows_at(pg1, st * 32 + 16), oV, v1p);
-        if (st + 4 < s_end) { nx0 = page_of(st * 32 + 128); nx1 = page_of(st * 32 + 144); }
-      }
-      for (; st < s_end; st += 4) {
-        const int k0 = st * 32, kg = k0 + 4 * g;             // key 16 kb + e of this lane: kg + 16 kb + e
-        const bool more = st + 4 < s_end;
-        f32x4 s[RB][2];
-        vec8 kf[2][HD / 32];
-        // no barrier here: this wave's own loads.  K's have landed when only V's 2 NI, which were issued behind them, are under way
-        wait_loads<2 * NI>();
+        int nx0 = entry_of(st * 32 + 128), nx1 = entry_of(st * 32 + 144);    // of the next step's
+        wait_loads<4 * NI>();                                  // the queries are here: nothing in the loop waits for them
+        for (; st < s_end; st += 4) {
+          const int k0 = st * 32, kg = k0 + 4 * g;             // key 16 kb + e of this lane: kg + 16 kb + e
+          const bool more = st + 4 < s_end;
+          f32x4 s[RB][2];
+          // no barrier here: this wave's own loads.  K's have landed when only V's 2 NI, which were issued behind them, are under way
+          vec8 kf[HD / 16];                                  // fragment 2 kk + kb
+          uint32_t at[HD / 16];
 #pragma unroll
-        for (int kk = 0; kk < HD / 32; ++kk) {
-          kf[0][kk] = *reinterpret_cast<const vec8 *>(k0p + (rdK ^ (kk * 32)));
-          kf[1][kk] = *reinterpret_cast<const vec8 *>(k1p + (rdK ^ (kk * 32)));
-        }
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            s[b][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int kk = 0; kk < HD / 32; ++kk) s[b][kb] = P16::mma16(kf[kb][kk], qf[b][kk], s[b][kb]);
+          for (int f = 0; f < HD / 16; ++f) at[f] = ((f & 1) ? at_k1 : at_k0) ^ ((f >> 1) * 64);
+          wait_loads<2 * NI>();
+          read_rows(kf, at);
+          const int cur0 = pg0, cur1 = pg1;
+          if (more) {                                        // K's LDS is free: the next step's keys may come
+            pg0 = page_from(nx0, k0 + 128);
+            pg1 = page_from(nx1, k0 + 144);
+            load16(Kh + rows_at(pg0, k0 + 128), oK, k0p);
+            load16(Kh + rows_at(pg1, k0 + 144), oK, k1p);
+            nx0 = entry_of(k0 + 256);
+            nx1 = entry_of(k0 + 272);
           }
-        // K's LDS is free once its reads have returned: the next step's keys may come
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int cur0 = pg0, cur1 = pg1;
-        if (more) {
-          pg0 = nx0;
-          pg1 = nx1;
-          load16(Kh + rows_at(pg0, k0 + 128), oK, k0p);
-          load16(Kh + rows_at(pg1, k0 + 144), oK, k1p);
-          if (st + 8 < s_end) { nx0 = page_of(k0 + 256); nx1 = page_of(k0 + 272); }
-        }
-        const bool masked = cur0 < 0 || cur1 < 0 || mixed(k0);
-        vec8 pf[RB];
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-          if (MOD) {
-            const Modifier modified(a.scale, a.softcap, slope[b], pos[b] - kg);
+          for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+              s[b][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int kk = 0; kk < HD / 32; ++kk) s[b][kb] = P16::mma16(kf[2 * kk + kb], qf[b][kk], s[b][kb]);
+            }
+          const bool masked = cur0 < 0 || cur1 < 0 || mixed(k0);
+          vec8 pf[RB];
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            if (MOD) {
+              const Modifier modified(a.scale, a.softcap, slope[b], pos[b] - kg);
+#pragma unroll
+              for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][kb][e] = modified(s[b][kb][e], kb * 16 + e);
+            }
+            if (masked) {
+              const int lo = (window > 0 ? pos[b] - window + 1 : 0) - kg, hi = (pos[b] < limit - 1 ? pos[b] : limit - 1) - kg;
+#pragma unroll
+              for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int key = kb * 16 + e;                 // from kg on
+                  if (!(key >= lo && key <= hi && (kb ? cur1 : cur0) >= 0)) s[b][kb][e] = -INFINITY;
+                }
+            }
+            float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
+                             fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+            mx = max_xor32(max_xor16(mx));
+            const float m_new = fmaxf(m_run[b], mx);
+            const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
+            const float alpha = __builtin_amdgcn_exp2f((m_run[b] - ref) * c_exp), mb = ref * c_exp - P16::kLift;
+            m_run[b] = m_new;
+            float psum = 0.f;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s[b][kb][e] = modified(s[b][kb][e], kb * 16 + e);
+              for (int e = 0; e < 4; e += 2) {
+                typename P16::vec2 ph;
+                ph[0] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e] * c_exp - mb);
+                ph[1] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e + 1] * c_exp - mb);
+                psum = P16::sum2(ph, psum);
+                pf[b][kb * 4 + e] = ph[0];
+                pf[b][kb * 4 + e + 1] = ph[1];
+              }
+            l_run[b] = l_run[b] * alpha + psum;
+            unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);   // as below
+            asm volatile("" : "+s"(moved));
+            if (moved != 0) {
+#pragma unroll
+              for (int t = 0; t < HD / 16; ++t) o[b][t] *= alpha;
+            }
+          }
+          vec8 vf[HD / 16];
+          if (more) wait_loads<2 * NI>();                    // V's have landed when only the next K's are under way
+          else wait_loads<0>();
+#pragma unroll
+          for (int t = 0; t < HD / 16; t += 4) {
+            s16x4 half8[8];
+            uint32_t at_v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) at_v[u] = ((u & 1) ? at_v1 : at_v0) ^ ((t + (u >> 1)) * 32);
+            read_transposed(half8, at_v);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) vf[t + u] = join_halves<vec8>(half8[2 * u], half8[2 * u + 1]);
+          }
+          if (more) {
+            load16(Vh + rows_at(pg0, k0 + 128), oV, v0p);
+            load16(Vh + rows_at(pg1, k0 + 144), oV, v1p);
           }
           if (masked) {
-            const int lo = (window > 0 ? pos[b] - window + 1 : 0) - kg, hi = (pos[b] < limit - 1 ? pos[b] : limit - 1) - kg;
+            u32x4 keep;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int key = kb * 16 + e;                 // from kg on
-                if (!(key >= lo && key <= hi && (kb ? cur1 : cur0) >= 0)) s[b][kb][e] = -INFINITY;
-              }
-          }
-          float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
-                           fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
-          mx = max_xor32(max_xor16(mx));
-          const float m_new = fmaxf(m_run[b], mx);
-          const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
-          const float alpha = __builtin_amdgcn_exp2f((m_run[b] - ref) * c_exp), mb = ref * c_exp - P16::kLift;
-          m_run[b] = m_new;
-          float psum = 0.f;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-              typename P16::vec2 ph;
-              ph[0] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e] * c_exp - mb);
-              ph[1] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e + 1] * c_exp - mb);
-              psum = P16::sum2(ph, psum);
-              pf[b][kb * 4 + e] = ph[0];
-              pf[b][kb * 4 + e + 1] = ph[1];
+            for (int w = 0; w < 4; ++w) {                      // halves 2 w and 2 w + 1: keys 16 (w / 2) + 4 g + 2 (w % 2) and the next
+              const int key = (w >> 1) * 16 + (w & 1) * 2;
+              const bool page = ((w >> 1) ? cur1 : cur0) >= 0;
+              keep[w] = (page && key < limit - kg ? 0xFFFFu : 0u) | (page && key + 1 < limit - kg ? 0xFFFF0000u : 0u);
             }
-          l_run[b] = l_run[b] * alpha + psum;
-          unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);   // as below
-          asm volatile("" : "+s"(moved));
-          if (moved != 0) {
+            u16x2 worst = {0, 0};
 #pragma unroll
-            for (int t = 0; t < HD / 16; ++t) o[b][t] *= alpha;
+            for (int t = 0; t < HD / 16; ++t) vf[t] = __builtin_bit_cast(vec8, clean_fragment(__builtin_bit_cast(u32x4, vf[t]), keep, worst));
+            if (__builtin_amdgcn_ballot_w64(not_finite<OT>(worst)) != 0) {
+              odd = true;
+#pragma unroll
+              for (int t = 0; t < HD / 16; ++t) vf[t] = __builtin_bit_cast(vec8, finite_only<OT>(__builtin_bit_cast(u32x4, vf[t])));
+            }
           }
+#pragma unroll
+          for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+            for (int b = 0; b < RB; ++b) o[b][t] = P16::mma16(vf[t], pf[b], o[b][t]);
         }
-        vec8 vf[HD / 16];
-        if (more) wait_loads<2 * NI>();                      // V's have landed when only the next K's are under way
-        else wait_loads<0>();
-#pragma unroll
-        for (int t = 0; t < HD / 16; ++t) vf[t] = join_halves<vec8>(read_transposed(v0p + (rdV ^ (t * 16))), read_transposed(v1p + (rdV ^ (t * 16))));
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) {
-          load16(Vh + rows_at(pg0, k0 + 128), oV, v0p);
-          load16(Vh + rows_at(pg1, k0 + 144), oV, v1p);
-        }
-        if (masked) {
-          u32x4 keep;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {                      // halves 2 w and 2 w + 1: keys 16 (w / 2) + 4 g + 2 (w % 2) and the next
-            const int key = (w >> 1) * 16 + (w & 1) * 2;
-            const bool page = ((w >> 1) ? cur1 : cur0) >= 0;
-            keep[w] = (page && key < limit - kg ? 0xFFFFu : 0u) | (page && key + 1 < limit - kg ? 0xFFFF0000u : 0u);
-          }
-          u16x2 worst = {0, 0};
-#pragma unroll
-          for (int t = 0; t < HD / 16; ++t) vf[t] = __builtin_bit_cast(vec8, clean_fragment(__builtin_bit_cast(u32x4, vf[t]), keep, worst));
-          if (__builtin_amdgcn_ballot_w64(not_finite<OT>(worst)) != 0) {
-            odd = true;
-#pragma unroll
-            for (int t = 0; t < HD / 16; ++t) vf[t] = __builtin_bit_cast(vec8, finite_only<OT>(__builtin_bit_cast(u32x4, vf[t])));
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < HD / 16; ++t)
-#pragma unroll
-          for (int b = 0; b < RB; ++b) o[b][t] = P16::mma16(vf[t], pf[b], o[b][t]);
       }
       if (odd) {
         for (int i = (it.tile0 * 2 + wave) * 2; i < s_end * 2; i += i & 1 ? 7 : 1) {     // both halves of each of this wave's steps
@@ -428,14 +439,19 @@ void attention_paged_16_kernel(const PagedAttn a) {
   float m_run = -INFINITY, l_run = 0.f;
 
   // a wave stages the tile's keys 16 wave .. 16 wave + 15; all four groups' pages say which keys exist
+  struct Entries { int e[4]; };
   struct Pages { int own; unsigned there; };
-  auto pages_of = [&](int kt) __attribute__((always_inline)) {
-    Pages p;
-    p.there = 0;
-    p.own = -1;
+  auto entries_of = [&](int kt) __attribute__((always_inline)) {
+    Entries n;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n.e[q] = entry_of(kt * 64 + q * 16);
+    return n;
+  };
+  auto pages_from = [&](const Entries &n, int kt) __attribute__((always_inline)) {
+    Pages p = {-1, 0};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int page = page_of(kt * 64 + q * 16);
+      const int page = page_from(n.e[q], kt * 64 + q * 16);
       p.there |= page >= 0 ? 1u << q : 0u;
       p.own = q == wave ? page : p.own;
     }
@@ -475,11 +491,12 @@ void attention_paged_16_kernel(const PagedAttn a) {
     odd = odd || __builtin_amdgcn_ballot_w64(not_finite<OT>(worst)) != 0;
   };
   const int kt_end = it.tile1;
-  Pages cur = {-1, 0}, next = {-1, 0}, after = {-1, 0};
+  Pages cur = {-1, 0};
+  Entries ahead = entries_of(it.tile0);                       // of the next tile that is not under way
   if (it.tile0 < kt_end) {
-    cur = pages_of(it.tile0);
+    cur = pages_from(ahead, it.tile0);
     stage(it.tile0, cur.own, std::integral_constant<int, 0>{});
-    if (it.tile0 + 1 < kt_end) next = pages_of(it.tile0 + 1);
+    ahead = entries_of(it.tile0 + 1);
     if (cur.there != 15u || mixed(it.tile0 * 64, it.pos0, last)) clean(it.tile0, cur.own, std::integral_constant<int, 0>{});
   }
   __syncthreads();                                            // also waits for this wave's own loads
@@ -488,16 +505,16 @@ void attention_paged_16_kernel(const PagedAttn a) {
     constexpr int CUR = decltype(cur_tag)::value;
     const OT *const lK = CUR ? lK1 : lK0;
     const OT *const lV = CUR ? lV1 : lV0;
-    if (kt + 1 < kt_end) {
-      stage(kt + 1, next.own, std::integral_constant<int, CUR ^ 1>{});
-      if (kt + 2 < kt_end) after = pages_of(kt + 2);
-    }
+    const Pages next = pages_from(ahead, kt + 1);
+    if (kt + 1 < kt_end) stage(kt + 1, next.own, std::integral_constant<int, CUR ^ 1>{});
+    ahead = entries_of(kt + 2);
     const int k0 = kt * 64, kh = k0 + 4 * half;
     if (touched(k0)) {
       int atK = rdK, atV = rdV;                               // opaque: the 16 addresses of either stage are one instruction each to make,
       asm volatile("" : "+v"(atK), "+v"(atV));                // and registers that spill if they are kept over the loop
       f32x16 s[2];
       vec8 kf[2][HD / 16];
+      wait_lds();                                             // of the scalar loads: with one under way, no LDS read can be waited for alone
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -581,7 +598,6 @@ void attention_paged_16_kernel(const PagedAttn a) {
       }
     }
     cur = next;
-    next = after;
     if (kt + 1 < kt_end && (cur.there != 15u || mixed(k0 + 64, it.pos0, last))) clean(kt + 1, cur.own, std::integral_constant<int, CUR ^ 1>{});
     __syncthreads();                                          // the next tile has landed and everyone is done with this one
   };
@@ -600,7 +616,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
   // lane holds d = 32 t + 8 (e / 4) + 4 half + e % 4 of its row
   if (odd) {
     for (int kt = it.tile0; kt < kt_end; ++kt) {
-      if (pages_of(kt).there == 15u && !mixed(kt * 64, it.pos0, last)) continue;
+      if (pages_from(entries_of(kt), kt).there == 15u && !mixed(kt * 64, it.pos0, last)) continue;
       for (int k0 = kt * 64; k0 < kt * 64 + 64 && k0 < limit; k0 += 16) {
         const int page = page_of(k0);
         if (page < 0) continue;

@@ -1,10 +1,10 @@
 // The fp32 form of the attention over a paged cache, on v_mfma_f32_16x16x4_f32.  Work items, rows and masks as in attn_paged.hip;
 // arithmetic and operand layout as in attn_fp32.hip: both products transposed, so that a lane owns one row (lane % 16) and the
-// accumulators of S^T are the next contraction's operand; operands straight from memory, one group of 16 keys ahead.
+// accumulators of S^T are the next contraction's operand.
 //
-// A wave takes 16 rows.  Items of more than 32 rows: a wave per 16 rows, each over all keys, in two workgroups (the matrix work of an
-// item is 16 times that of the 16-bit types, and a step of short chunks has few items).  Items of up to 32 rows: one workgroup whose
-// waves take the same rows and every fourth group of keys, and meet in LDS.
+// A workgroup of eight waves takes 64 rows of an item: a wave has 16 of them and every second group of 16 keys.  Items of up to 32 rows:
+// all waves take the same 16 rows, one block after the other, and every eighth group.  The waves of the same rows meet in LDS.
+//
 #include <type_traits>
 
 #include "paged.h"
@@ -12,11 +12,13 @@
 namespace prism {
 
 template <int NB, bool MOD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB <= 4 ? 3 : 2)))
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NB <= 4 ? 4 : 2)))
 void attention_paged_fp32_kernel(const PagedAttn a) {
   constexpr int HD = 16 * NB;
-  __shared__ __align__(16) float lO[4][16][HD];
-  __shared__ float2 lml[4][16];
+  constexpr int W = 8;                                        // waves
+  constexpr int CH = HD / 4, RI = 64 / CH, NI = 16 / RI;      // 16-byte chunks of a row; rows of a load instruction, instructions for 16 rows
+  __shared__ __align__(16) float lO[W][16][HD];               // a wave's 16 keys, at the end its results
+  __shared__ float2 lml[W][16];
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
   const PlanItem it = load_const(a.items + item);
@@ -27,21 +29,32 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   const int last = it.pos0 + it.n_tok - 1, limit = last + 1 < cap_keys ? last + 1 : cap_keys;
   const int32_t *const table = a.table + (int64_t)it.seq * a.shape.max_pages;
   const float *const Kh = (const float *)a.K + ((int64_t)kvh * HD << a.page_shift), *const Vh = (const float *)a.V + ((int64_t)kvh * HD << a.page_shift);
-  auto page_of = [&](int k0) __attribute__((always_inline)) {
-    if (k0 >= limit) return -1;
-    const int p = load_const(table + (k0 >> a.page_shift));
-    return (unsigned)p < (unsigned)a.shape.n_pages ? p : -1;
+  // table entry of the 16 keys from k0 on (behind the last key, that key's), and the page that it gives, none: -1
+  auto entry_of = [&](int k0) __attribute__((always_inline)) { return load_const(table + ((k0 < limit ? k0 : limit - 1) >> a.page_shift)); };
+  auto page_from = [&](int entry, int k0) __attribute__((always_inline)) { return k0 < limit && (unsigned)entry < (unsigned)a.shape.n_pages ? entry : -1; };
+  // K goes through LDS of the wave's own: a lane's operand is four dimensions of key lane % 16, and fetched as that, every lane of a load
+  // would be in a line of its own.  Chunk c of row r stands at slot c ^ swizzle(r), so that the 16 rows of a read spread over all banks.
+  auto swizzle = [](int r) { return HD == 32 ? (r >> 1) & 7 : r & 15; };
+  float *const lK = &lO[wave][0][0];
+  const uint32_t oK = (lane / CH * HD + ((lane % CH) ^ swizzle(lane / CH)) * 4) * 4;    // bytes; instruction j: its bits flipped
+  auto load_k = [&](const float *src) __attribute__((always_inline)) {
+    const char *const s = reinterpret_cast<const char *>(src);
+    constexpr uint32_t kFlip = HD == 32 ? 64 : RI * 16;
+    auto one = [&](auto j) __attribute__((always_inline)) {
+      constexpr int J = decltype(j)::value, kBase = J / 4 * 4096, kOffset = J % 4 * 1024;
+      static_assert(kOffset < 4096, "the immediate offset has 12 bits and a sign, and a larger one wraps without a word");
+      if constexpr (J < NI)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(s + kBase + (oK ^ (J * kFlip))),
+                                         (__attribute__((address_space(3))) void *)(lK + kBase / 4), 16, kOffset, 0);
+    };
+    one(std::integral_constant<int, 0>{}); one(std::integral_constant<int, 1>{}); one(std::integral_constant<int, 2>{}); one(std::integral_constant<int, 3>{});
+    one(std::integral_constant<int, 4>{}); one(std::integral_constant<int, 5>{}); one(std::integral_constant<int, 6>{}); one(std::integral_constant<int, 7>{});
   };
-  struct Tile { f32x4 k[NB]; float v[4][NB]; int page; };
-  auto fetch = [&](int k0, Tile &t) __attribute__((always_inline)) {
-    t.page = page_of(k0);
-    const int64_t at = (int64_t)(t.page < 0 ? 0 : t.page) * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
-    const float *kp = Kh + at + c * HD + 4 * g;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) t.k[b] = *reinterpret_cast<const f32x4 *>(kp + 16 * b);
+  struct Values { float v[4][NB]; };                          // s: key 4 g + s, dimensions NB c ..
+  auto load_v = [&](const float *src, Values &t) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const float *vp = Vh + at + (4 * g + s) * HD + NB * c;
+      const float *vp = src + (4 * g + s) * HD + NB * c;
       if constexpr (NB == 2) {
         const float2 v = *reinterpret_cast<const float2 *>(vp);
         t.v[s][0] = v.x; t.v[s][1] = v.y;
@@ -54,14 +67,20 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       }
     }
   };
+  auto rows_at = [&](int page, int k0) __attribute__((always_inline)) {
+    return (int64_t)(page < 0 ? 0 : page) * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
+  };
   const bool shared = rows <= 32;
   if (row_begin >= rows) return;
   const int n_groups = (limit + 15) >> 4, g_end = it.tile1 * 4 < n_groups ? it.tile1 * 4 : n_groups;
-  const int g_first = it.tile0 * 4 + (shared ? wave : 0), g_step = shared ? 4 : 1;
-  const int blocks = ((rows < row_begin + 64 ? rows : row_begin + 64) + 15) / 16;
-  for (int rb = shared ? 0 : row_begin / 16 + wave; rb < blocks; rb += shared ? 1 : 4) {
+  // waves of the same rows, and which of them this one is
+  const int n_same = shared ? W : 2, same = shared ? wave : wave >> 2;
+  const int g_first = it.tile0 * 4 + same, g_step = n_same;
+  for (int turn = 0; turn < (shared ? (rows + 15) / 16 : 1); ++turn) {
+    const int rb = shared ? turn : row_begin / 16 + (wave & 3);
+    const bool active = rb * 16 < rows;
     const int r = rb * 16 + c < rows ? rb * 16 + c : rows - 1, tok = r / G, head = kvh * G + r - tok * G, pos = it.pos0 + tok;
-    const int r_last = rb * 16 + 15 < rows ? rb * 16 + 15 : rows - 1;
+    const int r_last = rb * 16 + 15 < rows ? rb * 16 + 15 : rows - 1;   // (a wave without rows has the last one again and no keys)
     const int b_first = it.pos0 + rb * 16 / G, b_last = it.pos0 + r_last / G;    // positions of the block's first and last row
     const float slope = MOD && a.slopes ? a.slopes[head] : 0.f;
     f32x4 qf[NB], o[NB];
@@ -70,8 +89,9 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       qf[b] = *reinterpret_cast<const f32x4 *>((const float *)a.Q + (int64_t)(it.row0 + tok) * a.q_stride + (int64_t)head * HD + 16 * b + 4 * g);
       o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    wait_loads<0>();                                         // the queries are here: nothing in the loop waits for them
     float m_run = -INFINITY, l_run = 0.f;
-    auto work = [&](int grp, const Tile &t) __attribute__((always_inline)) {
+    auto work = [&](int grp, int page, const f32x4 (&k)[NB], const Values &t) __attribute__((always_inline)) {
       const int k0 = grp * 16;
       if (k0 > b_last || (window > 0 && k0 + 15 <= b_first - window)) return;   // no row of the block sees a key of it
       f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
@@ -79,10 +99,10 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       for (int b = 0; b < NB; b += 2)
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[b][s], qf[b][s], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[b + 1][s], qf[b + 1][s], s1, 0, 0, 0);
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b][s], qf[b][s], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b + 1][s], qf[b + 1][s], s1, 0, 0, 0);
         }
-      const bool masked = t.page < 0 || k0 + 15 > b_first || k0 + 15 >= limit || (window > 0 && k0 <= b_last - window);
+      const bool masked = page < 0 || k0 + 15 > b_first || k0 + 15 >= limit || (window > 0 && k0 <= b_last - window);
       const int lo = window > 0 ? pos - window + 1 : 0, hi = pos < limit - 1 ? pos : limit - 1;
       float p[4], mx = -INFINITY;
       bool see[4];
@@ -94,12 +114,11 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
           if (a.softcap > 0.f) p[s] = a.softcap * tanhf(p[s] / a.softcap);
           p[s] -= slope * (float)(pos - key);
         }
-        see[s] = !masked || (t.page >= 0 && key >= lo && key <= hi);
+        see[s] = !masked || (page >= 0 && key >= lo && key <= hi);
         if (!see[s]) p[s] = -INFINITY;
         mx = fmaxf(mx, p[s]);
       }
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = max_xor32(max_xor16(mx));
       const float m_new = fmaxf(m_run, mx), ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
       const float alpha = expf(m_run - ref);
       m_run = m_new;
@@ -120,7 +139,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
         for (int b = 0; b < NB; ++b) {
           v[s][b] = t.v[s][b];
           // a weight of zero times a value that is not finite would reach the sum: values of keys that no row sees become zero
-          if (masked && (t.page < 0 || k0 + 4 * g + s >= limit)) v[s][b] = 0.f;
+          if (masked && (page < 0 || k0 + 4 * g + s >= limit)) v[s][b] = 0.f;
           odd = odd || !(fabsf(v[s][b]) < INFINITY);
         }
       if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
@@ -151,78 +170,74 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[s][b], p[s], o[b], 0, 0, 0);
     };
-    // two groups' registers in turn; the scheduling barriers keep a group's loads in front of the work on the group before
-    Tile cur, next;
-    int grp = g_first;
-    if (grp < g_end) fetch(grp * 16, cur);
-    for (; grp < g_end; grp += 2 * g_step) {
-      const bool two = grp + g_step < g_end;
-      if (two) fetch((grp + g_step) * 16, next);
-      __builtin_amdgcn_sched_barrier(0);
-      work(grp, cur);
-      if (grp + 2 * g_step < g_end) fetch((grp + 2 * g_step) * 16, cur);
-      __builtin_amdgcn_sched_barrier(0);
-      if (two) work(grp + g_step, next);
+    // A group's K is in LDS and its V in registers when its turn comes.  Its K goes to registers at once, and the next group's K and V are
+    // requested ahead of its work, K into the LDS that is free now; a group's page is looked up a group ahead of that.
+    Values cur, next;
+    int grp = active ? g_first : g_end, page = -1, ahead = -1;   // ahead: the next group's table entry
+    if (grp < g_end) {
+      page = page_from(entry_of(grp * 16), grp * 16);
+      load_k(Kh + rows_at(page, grp * 16));
+      load_v(Vh + rows_at(page, grp * 16), cur);
+      ahead = entry_of((grp + g_step) * 16);
     }
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
-    if (shared) {
-      // o[b][e] is dimension NB (4 g + e) + b of row c
-      __syncthreads();
+    auto step = [&](const Values &own, Values &other) __attribute__((always_inline)) {
+      f32x4 k[NB];
+      wait_loads<0>();
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        f32x4 y;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = o[(4 * j + q) % NB][(4 * j + q) / NB];
-        *reinterpret_cast<f32x4 *>(&lO[wave][c][NB * 4 * g + 4 * j]) = y;
-      }
-      if (g == 0) lml[wave][c] = make_float2(m_run, l_run);
-      __syncthreads();
-      for (int e = threadIdx.x; e < 16 * HD / 4; e += 256) {
-        const int rr = e / (HD / 4), d = e % (HD / 4) * 4, row = rb * 16 + rr;
-        if (row >= rows) continue;
-        float m = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, lml[w][rr].x);
-        const float ref = m == -INFINITY ? 0.f : m;
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float2 x = lml[w][rr];
-          if (x.x == -INFINITY) continue;                    // a wave without keys has nothing
-          const float f = expf(x.x - ref);
-          const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][rr][d]);
-          sum += f * x.y;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] += f * z[q];
-        }
-        const int t = row / G, h = kvh * G + row - t * G;
-        if (it.part0 < 0) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] / sum;
-          *reinterpret_cast<f32x4 *>((float *)a.out + (int64_t)(it.row0 + t) * a.out_stride + (int64_t)h * HD + d) = y;
-        } else {
-          const int64_t at = (int64_t)(it.part0 + row) * nkv + kvh;
-          *reinterpret_cast<f32x4 *>(a.part_O + at * HD + d) = y;
-          if (d == 0) a.part_ml[at] = make_float2(m, sum);
-        }
-      }
-      continue;
+      for (int b = 0; b < NB; ++b) k[b] = *reinterpret_cast<const f32x4 *>(lK + c * HD + ((4 * b + g) ^ swizzle(c)) * 4);
+      const int next_grp = grp + g_step, page_own = page;
+      page = page_from(ahead, next_grp * 16);
+      if (next_grp < g_end) load_v(Vh + rows_at(page, next_grp * 16), other);
+      wait_lds();
+      if (next_grp < g_end) load_k(Kh + rows_at(page, next_grp * 16));
+      ahead = entry_of((next_grp + g_step) * 16);
+      __builtin_amdgcn_sched_barrier(0);
+      work(grp, page_own, k, own);
+      grp = next_grp;
+    };
+    while (grp < g_end) {
+      step(cur, next);
+      if (grp < g_end) step(next, cur);
     }
-    if (rb * 16 + c >= rows) continue;
-    const int64_t at = (int64_t)(it.part0 + rb * 16 + c) * nkv + kvh;
-    float *op = it.part0 < 0 ? (float *)a.out + (int64_t)(it.row0 + tok) * a.out_stride + (int64_t)head * HD : a.part_O + at * HD;
+    const float l_tot = sum_xor32(sum_xor16(l_run));
+    // o[b][e] is dimension NB (4 g + e) + b of row c; this wave's keys have been read
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       f32x4 y;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        y[q] = o[(4 * j + q) % NB][(4 * j + q) / NB];
-        if (it.part0 < 0) y[q] = l_run == 0.f ? 0.f : y[q] / l_run;
-      }
-      *reinterpret_cast<f32x4 *>(op + NB * 4 * g + 4 * j) = y;
+      for (int q = 0; q < 4; ++q) y[q] = o[(4 * j + q) % NB][(4 * j + q) / NB];
+      *reinterpret_cast<f32x4 *>(&lO[wave][c][NB * 4 * g + 4 * j]) = y;
     }
-    if (it.part0 >= 0 && g == 0) a.part_ml[at] = make_float2(m_run, l_run);
+    if (g == 0) lml[wave][c] = make_float2(m_run, l_tot);
+    __syncthreads();
+    for (int e = threadIdx.x; e < (shared ? 16 : 64) * HD / 4; e += 64 * W) {
+      const int rr = e / (HD / 4), d = e % (HD / 4) * 4, row = (shared ? turn * 16 : row_begin) + rr, w0 = rr >> 4, r16 = rr & 15;
+      if (row >= rows) continue;
+      float m = -INFINITY, sum = 0.f;
+      for (int w = w0; w < W; w += W / n_same) m = fmaxf(m, lml[w][r16].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      for (int w = w0; w < W; w += W / n_same) {
+        const float2 x = lml[w][r16];
+        if (x.x == -INFINITY) continue;                      // a wave without keys has nothing
+        const float f = expf(x.x - ref);
+        const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][r16][d]);
+        sum += f * x.y;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] += f * z[q];
+      }
+      const int t = row / G, h = kvh * G + row - t * G;
+      if (it.part0 < 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] / sum;
+        *reinterpret_cast<f32x4 *>((float *)a.out + (int64_t)(it.row0 + t) * a.out_stride + (int64_t)h * HD + d) = y;
+      } else {
+        const int64_t at = (int64_t)(it.part0 + row) * nkv + kvh;
+        *reinterpret_cast<f32x4 *>(a.part_O + at * HD + d) = y;
+        if (d == 0) a.part_ml[at] = make_float2(m, sum);
+      }
+    }
+    __syncthreads();                                          // the next block's keys may come
   }
 }
 
@@ -231,8 +246,8 @@ int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s) {
   const bool mod = a.softcap > 0.f || a.slopes;
   auto run = [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
-    if (mod) attention_paged_fp32_kernel<NB, true><<<dim3(grid, kPlanRows / 64), 256, 0, s>>>(a);
-    else attention_paged_fp32_kernel<NB, false><<<dim3(grid, kPlanRows / 64), 256, 0, s>>>(a);
+    if (mod) attention_paged_fp32_kernel<NB, true><<<dim3(grid, kPlanRows / 64), 512, 0, s>>>(a);
+    else attention_paged_fp32_kernel<NB, false><<<dim3(grid, kPlanRows / 64), 512, 0, s>>>(a);
   };
   if (hd == 32) run(std::integral_constant<int, 2>{});
   else if (hd == 64) run(std::integral_constant<int, 4>{});

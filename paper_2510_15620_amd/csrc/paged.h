@@ -17,7 +17,7 @@ namespace prism {
 // which is what bounds a launch's grid and the room for partial results without the host knowing a length.
 static const int kPlanRows = 128;        // query rows of a block
 static const int kPlanTile = 64;         // keys of a tile
-static const int kPlanItems = 1024;      // items wanted over all KV heads: two workgroups on each of 256 compute units, twice
+static const int kPlanItems = 1024;      // items wanted over all KV heads: twice the two workgroups that each of 256 compute units holds
 static const int kPlanMinTiles = 4;      // tiles of an item at least, where that leaves fewer items than wanted
 static const int kPlanNarrow = 32;       // rows of a sequence whose keys are cut freely
 static const int kPlanMinWide = 8;       // the same for the others
@@ -77,6 +77,16 @@ int check_kv_cache(const prism_kv_cache *c, const char *who);
 template <typename T> __device__ __forceinline__ T round_to(float v) { return from_f32<T>(v); }
 template <> __device__ __forceinline__ f16 round_to<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }
 
+// max of v over lanes l, l ^ 16 / l, l ^ 32
+__device__ __forceinline__ float max_xor32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_xor16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // A value that nothing writes while the kernel runs, at an address that is the same for the whole wave: by the scalar unit, so that
 // waiting for it is not waiting for the loads of K and V that are under way
 template <typename T> __device__ __forceinline__ T load_const(const T *p) {
@@ -85,6 +95,20 @@ template <typename T> __device__ __forceinline__ T load_const(const T *p) {
 #pragma unroll
   for (int i = 0; i < (int)(sizeof(T) / 4); ++i) u.w[i] = ((Words)(uintptr_t)p)[i];
   return u.v;
+}
+
+// Until at most N of this wave's memory accesses are under way.  They end in their order; others among them only make it wait longer.
+// By the builtin, so that the compiler knows which loads are done and does not wait for them again, with newer ones under way
+template <int N> __device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);      // vector loads; others: no wait
+  asm volatile("" ::: "memory");
+}
+// Until this wave's LDS reads have returned, so that what they read may be written again
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 3 << 14);
+  asm volatile("" ::: "memory");
 }
 
 // What an attention launch reads and writes.  Partial results of part row i and KV head h: values at O[(i * n_kv + h) * hd], running
