@@ -2,20 +2,24 @@
 // arithmetic and operand layout as in attn_fp32.hip: both products transposed, so that a lane owns one row (lane % 16) and the
 // accumulators of S^T are the next contraction's operand.
 //
-// A workgroup of eight waves takes 64 rows of an item: a wave has 16 of them and every second group of 16 keys.  Items of up to 32 rows:
-// all waves take the same 16 rows, one block after the other, and every eighth group.  The waves of the same rows meet in LDS.
-//
+// A workgroup of four waves takes 32 rows of an item.  Every wave has all of them, as two blocks of 16 that share a group of 16 keys in
+// registers, and every fourth group; the four meet in LDS.  What bounds it is the way from the L2 caches, since every wave fetches its
+// keys for itself: us of 40 ragged chunks over up to 900 keys, 4 heads of 64, with 16 rows per wave 76 (62 without either product), with
+// 32 70 (head size 128, where two blocks spill: 16 164, 32 285).
 #include <type_traits>
 
 #include "paged.h"
 
 namespace prism {
 
+// (head size 128: two blocks of rows would not fit the registers)
+constexpr int fp32_rows(int nb) { return nb <= 4 ? 32 : 16; }
+
 template <int NB, bool MOD>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NB <= 4 ? 4 : 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NB <= 4 ? 3 : 2)))
 void attention_paged_fp32_kernel(const PagedAttn a) {
   constexpr int HD = 16 * NB;
-  constexpr int W = 8;                                        // waves
+  constexpr int W = 4, kRows = fp32_rows(NB);                 // waves; rows of a workgroup
   constexpr int CH = HD / 4, RI = 64 / CH, NI = 16 / RI;      // 16-byte chunks of a row; rows of a load instruction, instructions for 16 rows
   __shared__ __align__(16) float lO[W][16][HD];               // a wave's 16 keys, at the end its results
   __shared__ float2 lml[W][16];
@@ -25,7 +29,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   const PlanHeader plan = load_const(a.plan);
   if (plan.magic != kPlanMagic || !same_shape(plan.shape, a.shape) || item >= plan.n_items) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int rows = it.n_tok * G, row_begin = blockIdx.y * 64, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
+  const int rows = it.n_tok * G, row_begin = blockIdx.y * kRows, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
   const int last = it.pos0 + it.n_tok - 1, limit = last + 1 < cap_keys ? last + 1 : cap_keys;
   const int32_t *const table = a.table + (int64_t)it.seq * a.shape.max_pages;
   const float *const Kh = (const float *)a.K + ((int64_t)kvh * HD << a.page_shift), *const Vh = (const float *)a.V + ((int64_t)kvh * HD << a.page_shift);
@@ -70,154 +74,165 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   auto rows_at = [&](int page, int k0) __attribute__((always_inline)) {
     return (int64_t)(page < 0 ? 0 : page) * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
   };
-  const bool shared = rows <= 32;
   if (row_begin >= rows) return;
   const int n_groups = (limit + 15) >> 4, g_end = it.tile1 * 4 < n_groups ? it.tile1 * 4 : n_groups;
-  // waves of the same rows, and which of them this one is
-  const int n_same = shared ? W : 2, same = shared ? wave : wave >> 2;
-  const int g_first = it.tile0 * 4 + same, g_step = n_same;
-  for (int turn = 0; turn < (shared ? (rows + 15) / 16 : 1); ++turn) {
-    const int rb = shared ? turn : row_begin / 16 + (wave & 3);
-    const bool active = rb * 16 < rows;
-    const int r = rb * 16 + c < rows ? rb * 16 + c : rows - 1, tok = r / G, head = kvh * G + r - tok * G, pos = it.pos0 + tok;
-    const int r_last = rb * 16 + 15 < rows ? rb * 16 + 15 : rows - 1;   // (a wave without rows has the last one again and no keys)
-    const int b_first = it.pos0 + rb * 16 / G, b_last = it.pos0 + r_last / G;    // positions of the block's first and last row
-    const float slope = MOD && a.slopes ? a.slopes[head] : 0.f;
-    f32x4 qf[NB], o[NB];
+  const int g_first = it.tile0 * 4 + wave;
+  constexpr int RB = kRows / 16;
+  const bool both = RB > 1 && row_begin + 16 < rows;
+  int pos[RB], b_first[RB], b_last[RB];                       // b_first, b_last: positions of a block's first and last row
+  float slope[RB], m_run[RB], l_run[RB];
+  f32x4 qf[RB][NB], o[RB][NB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i) {
+    const int r0 = row_begin + i * 16 < rows ? row_begin + i * 16 : rows - 1, r_last = r0 + 15 < rows ? r0 + 15 : rows - 1;
+    const int r = r0 + c < rows ? r0 + c : rows - 1, tok = r / G, head = kvh * G + r - tok * G;
+    pos[i] = it.pos0 + tok;
+    b_first[i] = it.pos0 + r0 / G;
+    b_last[i] = it.pos0 + r_last / G;
+    slope[i] = MOD && a.slopes ? a.slopes[head] : 0.f;
+    m_run[i] = -INFINITY;
+    l_run[i] = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      qf[b] = *reinterpret_cast<const f32x4 *>((const float *)a.Q + (int64_t)(it.row0 + tok) * a.q_stride + (int64_t)head * HD + 16 * b + 4 * g);
-      o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      qf[i][b] = *reinterpret_cast<const f32x4 *>((const float *)a.Q + (int64_t)(it.row0 + tok) * a.q_stride + (int64_t)head * HD + 16 * b + 4 * g);
+      o[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    wait_loads<0>();                                         // the queries are here: nothing in the loop waits for them
-    float m_run = -INFINITY, l_run = 0.f;
-    auto work = [&](int grp, int page, const f32x4 (&k)[NB], const Values &t) __attribute__((always_inline)) {
-      const int k0 = grp * 16;
-      if (k0 > b_last || (window > 0 && k0 + 15 <= b_first - window)) return;   // no row of the block sees a key of it
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+  }
+  wait_loads<0>();                                            // the queries are here: nothing in the loop waits for them
+  auto work = [&](auto block, int grp, int page, const f32x4 (&k)[NB], const Values &t) __attribute__((always_inline)) {
+    constexpr int I = decltype(block)::value;
+    const int k0 = grp * 16;
+    if (k0 > b_last[I] || (window > 0 && k0 + 15 <= b_first[I] - window)) return;   // no row of the block sees a key of it
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int b = 0; b < NB; b += 2)
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b][s], qf[b][s], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b + 1][s], qf[b + 1][s], s1, 0, 0, 0);
-        }
-      const bool masked = page < 0 || k0 + 15 > b_first || k0 + 15 >= limit || (window > 0 && k0 <= b_last - window);
-      const int lo = window > 0 ? pos - window + 1 : 0, hi = pos < limit - 1 ? pos : limit - 1;
-      float p[4], mx = -INFINITY;
-      bool see[4];
+    for (int b = 0; b < NB; b += 2)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const int key = k0 + 4 * g + s;
-        p[s] = (s0[s] + s1[s]) * a.scale;
-        if (MOD) {
-          if (a.softcap > 0.f) p[s] = a.softcap * tanhf(p[s] / a.softcap);
-          p[s] -= slope * (float)(pos - key);
-        }
-        see[s] = !masked || (page >= 0 && key >= lo && key <= hi);
-        if (!see[s]) p[s] = -INFINITY;
-        mx = fmaxf(mx, p[s]);
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b][s], qf[I][b][s], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b + 1][s], qf[I][b + 1][s], s1, 0, 0, 0);
       }
-      mx = max_xor32(max_xor16(mx));
-      const float m_new = fmaxf(m_run, mx), ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
-      const float alpha = expf(m_run - ref);
-      m_run = m_new;
-      float sum = 0.f;
+    const bool masked = page < 0 || k0 + 15 > b_first[I] || k0 + 15 >= limit || (window > 0 && k0 <= b_last[I] - window);
+    const int lo = window > 0 ? pos[I] - window + 1 : 0, hi = pos[I] < limit - 1 ? pos[I] : limit - 1;
+    float p[4], mx = -INFINITY;
+    bool see[4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        p[s] = expf(p[s] - ref);
-        sum += p[s];
+    for (int s = 0; s < 4; ++s) {
+      const int key = k0 + 4 * g + s;
+      p[s] = (s0[s] + s1[s]) * a.scale;
+      if (MOD) {
+        if (a.softcap > 0.f) p[s] = a.softcap * tanhf(p[s] / a.softcap);
+        p[s] -= slope[I] * (float)(pos[I] - key);
       }
-      l_run = l_run * alpha + sum;
+      see[s] = !masked || (page >= 0 && key >= lo && key <= hi);
+      if (!see[s]) p[s] = -INFINITY;
+      mx = fmaxf(mx, p[s]);
+    }
+    mx = max_xor32(max_xor16(mx));
+    const float m_new = fmaxf(m_run[I], mx), ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
+    const float alpha = expf(m_run[I] - ref);
+    m_run[I] = m_new;
+    float sum = 0.f;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) o[b] *= alpha;
-      float v[4][NB];
-      bool odd = false;
+    for (int s = 0; s < 4; ++s) {
+      p[s] = expf(p[s] - ref);
+      sum += p[s];
+    }
+    l_run[I] = l_run[I] * alpha + sum;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+    for (int b = 0; b < NB; ++b) o[I][b] *= alpha;
+    float v[4][NB];
+    bool odd = false;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        v[s][b] = t.v[s][b];
+        // a weight of zero times a value that is not finite would reach the sum: values of keys that no row sees become zero
+        if (masked && (page < 0 || k0 + 4 * g + s >= limit)) v[s][b] = 0.f;
+        odd = odd || !(fabsf(v[s][b]) < INFINITY);
+      }
+    if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
+      // those of keys that some rows see and others do not go to the rows that see them by indicators
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          v[s][b] = t.v[s][b];
-          // a weight of zero times a value that is not finite would reach the sum: values of keys that no row sees become zero
-          if (masked && (page < 0 || k0 + 4 * g + s >= limit)) v[s][b] = 0.f;
-          odd = odd || !(fabsf(v[s][b]) < INFINITY);
-        }
-      if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
-        // those of keys that some rows see and others do not go to the rows that see them by indicators
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {
-          const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+          f32x4 n = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            f32x4 n = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-              const float x = v[s][b];
-              const bool is = kind == 2 ? x != x : x == add;
-              n = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.0f : 0.0f, see[s] ? 1.0f : 0.0f, n, 0, 0, 0);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[b][e] += n[e] > 0.f ? add : 0.f;
+          for (int s = 0; s < 4; ++s) {
+            const float x = v[s][b];
+            const bool is = kind == 2 ? x != x : x == add;
+            n = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.0f : 0.0f, see[s] ? 1.0f : 0.0f, n, 0, 0, 0);
           }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[I][b][e] += n[e] > 0.f ? add : 0.f;
         }
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int b = 0; b < NB; ++b) v[s][b] = fabsf(v[s][b]) < INFINITY ? v[s][b] : 0.f;
       }
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[s][b], p[s], o[b], 0, 0, 0);
-    };
-    // A group's K is in LDS and its V in registers when its turn comes.  Its K goes to registers at once, and the next group's K and V are
-    // requested ahead of its work, K into the LDS that is free now; a group's page is looked up a group ahead of that.
-    Values cur, next;
-    int grp = active ? g_first : g_end, page = -1, ahead = -1;   // ahead: the next group's table entry
-    if (grp < g_end) {
-      page = page_from(entry_of(grp * 16), grp * 16);
-      load_k(Kh + rows_at(page, grp * 16));
-      load_v(Vh + rows_at(page, grp * 16), cur);
-      ahead = entry_of((grp + g_step) * 16);
+        for (int b = 0; b < NB; ++b) v[s][b] = fabsf(v[s][b]) < INFINITY ? v[s][b] : 0.f;
     }
-    auto step = [&](const Values &own, Values &other) __attribute__((always_inline)) {
-      f32x4 k[NB];
-      wait_loads<0>();
 #pragma unroll
-      for (int b = 0; b < NB; ++b) k[b] = *reinterpret_cast<const f32x4 *>(lK + c * HD + ((4 * b + g) ^ swizzle(c)) * 4);
-      const int next_grp = grp + g_step, page_own = page;
-      page = page_from(ahead, next_grp * 16);
-      if (next_grp < g_end) load_v(Vh + rows_at(page, next_grp * 16), other);
-      wait_lds();
-      if (next_grp < g_end) load_k(Kh + rows_at(page, next_grp * 16));
-      ahead = entry_of((next_grp + g_step) * 16);
-      __builtin_amdgcn_sched_barrier(0);
-      work(grp, page_own, k, own);
-      grp = next_grp;
-    };
-    while (grp < g_end) {
-      step(cur, next);
-      if (grp < g_end) step(next, cur);
-    }
-    const float l_tot = sum_xor32(sum_xor16(l_run));
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) o[I][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[s][b], p[s], o[I][b], 0, 0, 0);
+  };
+  // A group's K is in LDS and its V in registers when its turn comes.  Its K goes to registers at once, and the next group's K and V are
+  // requested ahead of its work, K into the LDS that is free now; a group's page is looked up a group ahead of that.
+  Values cur, next;
+  int grp = g_first, page = -1, ahead = -1;   // ahead: the next group's table entry
+  if (grp < g_end) {
+    page = page_from(entry_of(grp * 16), grp * 16);
+    load_k(Kh + rows_at(page, grp * 16));
+    load_v(Vh + rows_at(page, grp * 16), cur);
+    ahead = entry_of((grp + W) * 16);
+  }
+  auto step = [&](const Values &own, Values &other) __attribute__((always_inline)) {
+    f32x4 k[NB];
+    wait_loads<0>();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) k[b] = *reinterpret_cast<const f32x4 *>(lK + c * HD + ((4 * b + g) ^ swizzle(c)) * 4);
+    const int next_grp = grp + W, page_own = page;
+    page = page_from(ahead, next_grp * 16);
+    if (next_grp < g_end) load_v(Vh + rows_at(page, next_grp * 16), other);
+    wait_lds();
+    if (next_grp < g_end) load_k(Kh + rows_at(page, next_grp * 16));
+    ahead = entry_of((next_grp + W) * 16);
+    __builtin_amdgcn_sched_barrier(0);
+    work(std::integral_constant<int, 0>{}, grp, page_own, k, own);
+    if (both) work(std::integral_constant<int, RB - 1>{}, grp, page_own, k, own);
+    grp = next_grp;
+  };
+  while (grp < g_end) {
+    step(cur, next);
+    if (grp < g_end) step(next, cur);
+  }
+#pragma unroll
+  for (int i = 0; i < RB; ++i) {
+    if (row_begin + i * 16 >= rows) break;
+    const float l_tot = sum_xor32(sum_xor16(l_run[i]));
     // o[b][e] is dimension NB (4 g + e) + b of row c; this wave's keys have been read
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       f32x4 y;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) y[q] = o[(4 * j + q) % NB][(4 * j + q) / NB];
+      for (int q = 0; q < 4; ++q) y[q] = o[i][(4 * j + q) % NB][(4 * j + q) / NB];
       *reinterpret_cast<f32x4 *>(&lO[wave][c][NB * 4 * g + 4 * j]) = y;
     }
-    if (g == 0) lml[wave][c] = make_float2(m_run, l_tot);
+    if (g == 0) lml[wave][c] = make_float2(m_run[i], l_tot);
     __syncthreads();
-    for (int e = threadIdx.x; e < (shared ? 16 : 64) * HD / 4; e += 64 * W) {
-      const int rr = e / (HD / 4), d = e % (HD / 4) * 4, row = (shared ? turn * 16 : row_begin) + rr, w0 = rr >> 4, r16 = rr & 15;
+    for (int e = threadIdx.x; e < 16 * HD / 4; e += 64 * W) {
+      const int r16 = e / (HD / 4), d = e % (HD / 4) * 4, row = row_begin + i * 16 + r16;
       if (row >= rows) continue;
       float m = -INFINITY, sum = 0.f;
-      for (int w = w0; w < W; w += W / n_same) m = fmaxf(m, lml[w][r16].x);
+#pragma unroll
+      for (int w = 0; w < W; ++w) m = fmaxf(m, lml[w][r16].x);
       const float ref = m == -INFINITY ? 0.f : m;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
-      for (int w = w0; w < W; w += W / n_same) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
         const float2 x = lml[w][r16];
         if (x.x == -INFINITY) continue;                      // a wave without keys has nothing
         const float f = expf(x.x - ref);
@@ -237,7 +252,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
         if (d == 0) a.part_ml[at] = make_float2(m, sum);
       }
     }
-    __syncthreads();                                          // the next block's keys may come
+    __syncthreads();                                          // the next block's results may come
   }
 }
 
@@ -246,8 +261,8 @@ int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s) {
   const bool mod = a.softcap > 0.f || a.slopes;
   auto run = [&](auto nb) {
     constexpr int NB = decltype(nb)::value;
-    if (mod) attention_paged_fp32_kernel<NB, true><<<dim3(grid, kPlanRows / 64), 512, 0, s>>>(a);
-    else attention_paged_fp32_kernel<NB, false><<<dim3(grid, kPlanRows / 64), 512, 0, s>>>(a);
+    if (mod) attention_paged_fp32_kernel<NB, true><<<dim3(grid, kPlanRows / fp32_rows(NB)), 256, 0, s>>>(a);
+    else attention_paged_fp32_kernel<NB, false><<<dim3(grid, kPlanRows / fp32_rows(NB)), 256, 0, s>>>(a);
   };
   if (hd == 32) run(std::integral_constant<int, 2>{});
   else if (hd == 64) run(std::integral_constant<int, 4>{});
