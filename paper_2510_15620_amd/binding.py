@@ -393,30 +393,36 @@ def _need(ok: bool, what: str):
         raise PrismError(EINVAL, what)
 
 
-def _ints(device: int, **tensors):
-    """Addresses of dense int32 device tensors; name=(tensor, values that it has to hold)."""
-    import torch
-    i32, out = torch.int32, []
-    for t, n in tensors.values():
-        if t.dtype is not i32 or t.numel() < n or not t.is_contiguous() or t.get_device() != device:
-            name = next(k for k, v in tensors.items() if v[0] is t)
-            raise PrismError(EINVAL, f"{name}: a dense int32 tensor of {n} values on the current device")
-        out.append(t.data_ptr())
-    return out
+def _ints(t, n: int, device: int, what: str) -> int:
+    """Address of a dense int32 device tensor of at least n values."""
+    if t.dtype is _torch.int32 and t.numel() >= n and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    raise PrismError(EINVAL, f"{what}: a dense int32 tensor of {n} values on the current device")
 
 
-def _rows(t, n: int, width: int, dtype, device: int, what: str):
-    """Address and row stride of an [n, width] device tensor whose rows are dense."""
-    if t.shape != (n, width) or t.dtype is not dtype or t.get_device() != device or (t.stride(1) != 1 and width > 1):
-        raise PrismError(EINVAL, f"{what}: [{n}, {width}] of {dtype}, rows dense, on the current device")
-    return t.data_ptr(), t.stride(0) if n > 1 else width
+def _rows(t, dtype, device: int, what: str):
+    """Address, row stride, rows and width of a two-dimensional device tensor whose rows are dense."""
+    if t.dim() == 2 and t.dtype is dtype and t.get_device() == device:
+        n, width = t.shape
+        stride, one = t.stride()
+        if one == 1 or width < 2:
+            return t.data_ptr(), stride if n > 1 else width, n, width
+    raise PrismError(EINVAL, f"{what}: rows of {dtype}, dense, on the current device")
+
+
+def _gain(t, hd: int, dtype, device: int) -> int:
+    if t is not None and t.dtype is dtype and t.numel() == hd and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    raise PrismError(EINVAL, f"a gain of {hd} values of {dtype} on the current device")
+
+
+_torch = None               # set with the first cache or plan: the calls below have both at hand and are short
 
 
 def _here():
-    """Current device and its current stream."""
-    import torch
-    d = torch.cuda.current_device()
-    return d, torch._C._cuda_getCurrentRawStream(d)          # the stream's handle without making a Stream object
+    """Current device and its current stream's handle (without making a Stream object)."""
+    d = _torch.cuda.current_device()
+    return d, _torch._C._cuda_getCurrentRawStream(d)
 
 
 class KVCache:
@@ -424,7 +430,9 @@ class KVCache:
     from page to page is free, and the same for both (K and V may be views into one allocation)."""
 
     def __init__(self, K, V):
+        global _torch
         import torch
+        _torch = torch
         _need(K.dim() == 4 and K.shape == V.shape and K.dtype is V.dtype and K.is_cuda and K.device == V.device, "KVCache: K and V alike")
         n, heads, size, hd = K.shape
         _need(K.dtype in (torch.float32, torch.bfloat16, torch.float16), "KVCache: fp32, bf16 or half")
@@ -444,7 +452,9 @@ class PagePlan:
 
     def __init__(self, n_seqs: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, page_size: int, n_pages: int, max_pages: int,
                  window: int = 0):
+        global _torch
         import torch
+        _torch = torch
         self._c = prism_page_shape(n_seqs, n_tokens, n_q_heads, n_kv_heads, page_size, n_pages, max_pages, window)
         self._ref = C.byref(self._c)
         size = int(lib().prism_page_plan_bytes(self._ref))
@@ -454,38 +464,35 @@ class PagePlan:
         self.buffer = torch.zeros(size, dtype=torch.uint8, device="cuda")
         self.device = self.buffer.get_device()
 
-    @property
-    def address(self):
-        return self.buffer.data_ptr()
-
 
 def op_page_plan(plan: PagePlan, cached, fresh, table, free_pages, n_free, n_free_left, cu, pos, slot, status=None):
     """cached, fresh [n_seqs]; table [n_seqs, max_pages]; free_pages [any]; n_free, n_free_left [1]; cu [n_seqs + 1]; pos, slot
     [n_tokens]; status [4] or None: int32 device tensors."""
-    (d, stream), n, T = _here(), plan.n_seqs, plan.n_tokens
-    _need(plan.device == d, "op_page_plan: the plan is on another device than the current one")
-    cached, fresh, table, pages, *out = _ints(
-        d, cached=(cached, n), fresh=(fresh, n), table=(table, n * plan.max_pages), free_pages=(free_pages, 0), n_free=(n_free, 1),
-        n_free_left=(n_free_left, 1), cu=(cu, n + 1), pos=(pos, T), slot=(slot, T), **({} if status is None else {"status": (status, 4)}))
-    _check(lib().prism_op_page_plan(plan._ref, cached, fresh, table, pages, free_pages.numel(), *out, *(() if status is not None else (0,)),
-                                    plan.address, stream))
+    d, stream = _here()
+    n, T = plan.n_seqs, plan.n_tokens
+    if plan.device != d:
+        raise PrismError(EINVAL, "op_page_plan: the plan is on another device than the current one")
+    _check(lib().prism_op_page_plan(
+        plan._ref, _ints(cached, n, d, "cached"), _ints(fresh, n, d, "fresh"), _ints(table, n * plan.max_pages, d, "table"),
+        _ints(free_pages, 0, d, "free_pages"), free_pages.numel(), _ints(n_free, 1, d, "n_free"), _ints(n_free_left, 1, d, "n_free_left"),
+        _ints(cu, n + 1, d, "cu"), _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"),
+        0 if status is None else _ints(status, 4, d, "status"), plan.buffer.data_ptr(), stream))
 
 
 def op_qkv_finish_paged(QKV, pos, slot, cache: KVCache, q_gain, k_gain, eps, base, qk_norm, Q):
     """QKV [T, (nq + 2 nkv) * hd] fp32 or in the cache's dtype -> Q [T, nq * hd] and the cache's slots."""
-    import torch
-    (d, stream), hd, nkv = _here(), cache.head_dim, cache.n_kv_heads
-    T, nq = QKV.shape[0], Q.shape[1] // hd
-    _need(cache.device == d, "op_qkv_finish_paged: the cache is on another device than the current one")
-    x, x_stride = _rows(QKV, T, (nq + 2 * nkv) * hd, torch.float32 if QKV.dtype is torch.float32 else cache.dtype, d, "QKV")
-    at, slots = _ints(d, pos=(pos, T), slot=(slot, T))
-    q, q_stride = _rows(Q, T, nq * hd, cache.dtype, d, "Q")
-    if qk_norm:
-        for g in (q_gain, k_gain):
-            _need(g is not None and g.dtype is cache.dtype and g.numel() == hd and g.is_contiguous() and g.get_device() == d,
-                  "op_qkv_finish_paged: gains of head_dim values in the cache's dtype")
-    _check(lib().prism_op_qkv_finish_paged(cache._ref, DTYPE_FP32 if QKV.dtype is torch.float32 else cache._c.dtype, x, x_stride, T, at, slots, nq,
-                                           _ptr(q_gain), _ptr(k_gain), eps, base, int(qk_norm), q, q_stride, stream))
+    d, stream = _here()
+    hd, nkv, dtype = cache.head_dim, cache.n_kv_heads, cache.dtype
+    if cache.device != d:
+        raise PrismError(EINVAL, "op_qkv_finish_paged: the cache is on another device than the current one")
+    wide = QKV.dtype is _torch.float32
+    x, x_stride, T, x_width = _rows(QKV, _torch.float32 if wide else dtype, d, "QKV")
+    q, q_stride, q_rows, q_width = _rows(Q, dtype, d, "Q")
+    if q_rows != T or q_width % hd or x_width != q_width + 2 * nkv * hd:
+        raise PrismError(EINVAL, f"op_qkv_finish_paged: QKV [{T}, {x_width}], Q [{q_rows}, {q_width}], {nkv} KV heads of {hd}")
+    _check(lib().prism_op_qkv_finish_paged(
+        cache._ref, DTYPE_FP32 if wide else cache._c.dtype, x, x_stride, T, _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"), q_width // hd,
+        _gain(q_gain, hd, dtype, d) if qk_norm else 0, _gain(k_gain, hd, dtype, d) if qk_norm else 0, eps, base, 1 if qk_norm else 0, q, q_stride, stream))
 
 
 def attention_paged_workspace(plan: PagePlan, cache: KVCache):
@@ -499,15 +506,15 @@ def attention_paged_workspace(plan: PagePlan, cache: KVCache):
 
 def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace, scale: float = 0.0, softcap: float = 0.0, slopes=None):
     """Q, out [n_tokens, n_q_heads * hd] in the cache's dtype; table as op_page_plan left it; slopes [n_q_heads] fp32 or None."""
-    import torch
-    (d, stream), T, width = _here(), plan.n_tokens, plan.n_q_heads * cache.head_dim
-    _need(plan.device == d and cache.device == d and workspace.get_device() == d, "op_attention_paged: tensors on another device than the current one")
-    q, q_stride = _rows(Q, T, width, cache.dtype, d, "Q")
-    o, o_stride = _rows(out, T, width, cache.dtype, d, "out")
-    if slopes is not None:
-        _need(slopes.dtype is torch.float32 and slopes.numel() == plan.n_q_heads and slopes.is_contiguous() and slopes.get_device() == d,
-              "op_attention_paged: slopes of n_q_heads fp32 values")
-    pages, = _ints(d, table=(table, plan.n_seqs * plan.max_pages))
-    _need(workspace.is_contiguous(), "op_attention_paged: a dense workspace")
-    _check(lib().prism_op_attention_paged(plan._ref, cache._ref, plan.address, pages, q, q_stride, scale, softcap, _ptr(slopes), o, o_stride,
-                                          workspace.data_ptr(), workspace.nbytes, stream))
+    d, stream = _here()
+    if plan.device != d or cache.device != d or workspace.get_device() != d or not workspace.is_contiguous():
+        raise PrismError(EINVAL, "op_attention_paged: a plan, a cache and a dense workspace on the current device")
+    q, q_stride, T, width = _rows(Q, cache.dtype, d, "Q")
+    o, o_stride, o_rows, o_width = _rows(out, cache.dtype, d, "out")
+    if T != plan.n_tokens or o_rows != T or width != plan.n_q_heads * cache.head_dim or o_width != width:
+        raise PrismError(EINVAL, f"op_attention_paged: Q [{T}, {width}], out [{o_rows}, {o_width}] for {plan.n_tokens} rows of {plan.n_q_heads} heads")
+    if slopes is not None and (slopes.dtype is not _torch.float32 or slopes.numel() != plan.n_q_heads or not slopes.is_contiguous() or slopes.get_device() != d):
+        raise PrismError(EINVAL, "op_attention_paged: slopes of n_q_heads fp32 values")
+    _check(lib().prism_op_attention_paged(
+        plan._ref, cache._ref, plan.buffer.data_ptr(), _ints(table, plan.n_seqs * plan.max_pages, d, "table"), q, q_stride, scale, softcap,
+        0 if slopes is None else slopes.data_ptr(), o, o_stride, workspace.data_ptr(), workspace.nbytes, stream))
