@@ -361,7 +361,8 @@ int prism_op_qkv_finish_paged(const prism_kv_cache *cache, int32_t qkv_dtype, co
 
 /* Attention of the step's tokens over the cache, which holds their own keys and values already.  A query at position p sees the keys
  * of its sequence at positions k <= p (with a window: p - window < k) that have a page in the pool; scores are
- *   s = scale q.k (scale 0: 1 / sqrt(head_dim)),  softcap > 0: s = softcap tanh(s / softcap),  slopes: s -= slopes[head] (p - k),
+ *   s = scale q.k (scale 0: 1 / sqrt(head_dim)),  softcap > 0: s = softcap tanh(s / softcap),  slopes: s -= slopes[head] (p - k)
+ * (scale, softcap and scale / softcap below 1e37),
  * softmax over the keys seen, times V.  A query that sees no key gives zeros; rows behind the last sequence are not written.  Keys
  * and values that a query does not see never reach its result, whatever they hold (NaN and infinities included).
  *   shape, plan, table: those of prism_op_page_plan (with a plan of another shape nothing is written).  Q, out: n_tokens rows of

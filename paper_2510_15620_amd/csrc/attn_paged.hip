@@ -778,7 +778,9 @@ extern "C" int prism_op_attention_paged(const prism_page_shape *shape, const pri
   PRISM_TRY(check_kv_cache(cache, "attention_paged"));
   PRISM_REQUIRE(shape->n_kv_heads == cache->n_kv_heads && shape->page_size == cache->page_size && shape->n_pages == cache->n_pages, PRISM_EINVAL,
                 "attention_paged: the plan's pages are not the cache's");
-  PRISM_REQUIRE(scale >= 0.f && softcap >= 0.f && scale < INFINITY && softcap < INFINITY, PRISM_EINVAL, "attention_paged: scale %g, softcap %g", scale, softcap);
+  // (the factors that the kernels make of them, with log2(e) in them, have to be numbers too)
+  PRISM_REQUIRE(scale >= 0.f && softcap >= 0.f && scale < 1e37f && softcap < 1e37f &&
+                (softcap == 0.f || (scale > 0.f ? scale : 1.0f) / softcap < 1e37f), PRISM_EINVAL, "attention_paged: scale %g, softcap %g", scale, softcap);
   if (shape->n_tokens == 0 || shape->n_seqs == 0) return PRISM_OK;
   PRISM_REQUIRE(plan && table && Q && out && workspace, PRISM_EINVAL, "attention_paged: bad arguments");
   const int hd = cache->head_dim;

@@ -265,6 +265,31 @@ def test_attention_keeps_what_is_not_seen_out(dtype, hd, fresh):
     assert torch.isfinite(out[:2]).all()
 
 
+@pytest.mark.parametrize("dtype,nq,hd", [(F16, 8, 128), (BF16, 14, 64), (F32, 8, 64)])
+@pytest.mark.parametrize("fresh,window", [(1, 40), (3, 40), (8, 100), (60, 40), (150, 130)])
+def test_attention_window_drops_values_that_are_not_finite(dtype, nq, hd, fresh, window):
+    """Cached values and keys that are not finite, some behind the window of every token, some of a few, some of none."""
+    s = R.Step([200], [fresh], 16, nq, 2, hd, dtype, seed=fresh, window=window, stale=float("nan"))
+    first = 200 - window + 1                                     # the first position that the first token sees
+    for p, what, d in ((first - 70, float("nan"), 1), (first - 1, float("inf"), 2), (first, -float("inf"), 3), (first + 2, float("nan"), 4),
+                       (first + 5, float("inf"), 3), (199 + fresh // 2, float("inf"), 5)):
+        s.V[int(s.full_table[0, p // 16]), 0, p % 16, d] = what
+    s.K[int(s.full_table[0, (first - 1) // 16]), 1, (first - 1) % 16, 0] = float("inf")
+    s.make_plan()
+    out = s.attend()
+    ref, room = R.attend(s.Q, s.K, s.V, s.full_table, s.cached, s.cu, nq, 2, hd, window=window, dtype=dtype)
+    if dtype == F16:
+        ref = torch.where(torch.isinf(ref), torch.sign(ref) * 65504.0, ref)
+    R.close(out, ref, room)
+
+
+@pytest.mark.parametrize("dtype,nq,nkv,hd", [(F16, 128, 1, 128), (BF16, 256, 256, 64), (F16, 33, 1, 64), (F32, 96, 1, 32)])
+def test_attention_of_the_widest_head_groups(dtype, nq, nkv, hd):
+    s = R.Step([0, 70, 300], [3, 1, 20], 32, nq, nkv, hd, dtype, seed=nq, stale=float("nan"))
+    s.make_plan()
+    s.check()
+
+
 def test_attention_with_strided_rows_in_place_and_interleaved_pages():
     s = R.Step([100, 3], [40, 2], 32, 8, 2, 128, F16, seed=11, interleaved=True)
     s.make_plan()
@@ -418,3 +443,57 @@ def test_same_inputs_same_bits():
     first = s.attend()
     for _ in range(3):
         assert torch.equal(first, s.attend())
+
+
+def test_plan_of_the_largest_step():
+    """As many sequences and rows as a step may have."""
+    r = np.random.default_rng(1)
+    f = r.integers(0, 512, 4096)
+    f[7] += 1048576 - f.sum()
+    c = r.integers(0, 40, 4096)
+    has, need = -(-c // 64), -(-(c + f) // 64)
+    table = np.full((4096, int(need.max())), -1, np.int32)
+    order, at = r.permutation(int(need.sum())).astype(np.int32), 0
+    for s in range(4096):
+        table[s, : has[s]] = order[at: at + has[s]]
+        at += has[s]
+    _check_plan(c.astype(np.int32), f.astype(np.int32), table, order[at:], len(order) - at, 1048576, 64, len(order), 32, 8)
+
+
+def test_refusals_of_tensors():
+    """Types, shapes, strides and devices that do not fit are refused before anything is launched."""
+    s = R.Step([20], [3], 16, 4, 2, 64, F16)
+    out = s.make_plan()
+    ints = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)  # noqa: E731
+    good = [s.device(s.cached), s.device(s.fresh), s.d_table, s.device(s.free), s.device([len(s.free)]), out["left"], out["cu"], out["pos"], out["slot"]]
+    for i, bad in ((0, ints(1).long()), (1, ints(0)), (2, s.d_table.cpu()), (2, ints(0)), (4, ints(0)), (6, ints(1)), (7, ints(2)), (8, ints(6)[::2]), (5, ints(1).float())):
+        with pytest.raises(B.PrismError) as e:
+            B.op_page_plan(s.plan, *good[:i], bad, *good[i + 1:])
+        assert e.value.code == B.EINVAL
+    QKV, Q, g = torch.zeros(3, 8 * 64, device=DEV), torch.zeros(3, 4 * 64, dtype=F16, device=DEV), torch.ones(64, dtype=F16, device=DEV)
+    finish = lambda QKV=QKV, pos=out["pos"], slot=out["slot"], cache=s.cache, a=g, b=g, Q=Q: B.op_qkv_finish_paged(QKV, pos, slot, cache, a, b, 1e-6, 1e6, True, Q)  # noqa: E731
+    finish()
+    for bad in (dict(QKV=QKV.bfloat16()), dict(QKV=QKV[:, :500]), dict(QKV=QKV.T), dict(QKV=QKV[:2]), dict(QKV=QKV.cpu()), dict(pos=ints(2)), dict(slot=ints(3).long()),
+                dict(a=None), dict(b=g.float()), dict(a=g[:32]), dict(Q=Q.float()), dict(Q=torch.zeros(3, 250, dtype=F16, device=DEV)), dict(QKV=QKV.view(-1))):
+        with pytest.raises(B.PrismError) as e:
+            finish(**bad)
+        assert e.value.code == B.EINVAL, bad
+    ws = B.attention_paged_workspace(s.plan, s.cache)
+    attend = lambda Q=s.Q, table=s.d_table, o=Q, ws=ws, **more: B.op_attention_paged(s.plan, Q, s.cache, table, o, ws, **more)  # noqa: E731
+    attend()
+    for bad in (dict(Q=s.Q.bfloat16()), dict(Q=s.Q[:2]), dict(Q=s.Q[:, :128]), dict(o=Q.cpu()), dict(o=Q.T), dict(table=s.d_table.long()), dict(table=ints(1)), dict(ws=ws[:16]),
+                dict(ws=ws[1:]), dict(ws=ws.cpu()), dict(slopes=torch.zeros(3, device=DEV)), dict(slopes=torch.zeros(4, dtype=F16, device=DEV)), dict(scale=-1.0), dict(softcap=-2.0)):
+        with pytest.raises(B.PrismError) as e:
+            attend(**bad)
+        assert e.value.code == B.EINVAL, bad
+    for K, V in ((torch.zeros(2, 2, 16, 64, device=DEV), torch.zeros(2, 2, 16, 64, dtype=F16, device=DEV)), (torch.zeros(2, 2, 16, 64).half(), torch.zeros(2, 2, 16, 64).half()),
+                 (torch.zeros(2, 2, 64, 16, device=DEV).transpose(2, 3), torch.zeros(2, 2, 16, 64, device=DEV)), (torch.zeros(2, 2, 16, 64, device=DEV),) * 1 + (torch.zeros(3, 2, 16, 64, device=DEV),),
+                 (torch.zeros(2, 2, 16, 64, dtype=torch.float64, device=DEV),) * 2, (torch.zeros(2, 16, 64, device=DEV),) * 2):
+        with pytest.raises(B.PrismError):
+            B.KVCache(K, V)
+    for bad in (dict(n_seqs=-1), dict(page_size=24), dict(n_q_heads=5), dict(max_pages=0)):
+        v = dict(n_seqs=1, n_tokens=3, n_q_heads=4, n_kv_heads=2, page_size=16, n_pages=4, max_pages=2)
+        v.update(bad)
+        with pytest.raises(B.PrismError):
+            B.PagePlan(**v)
+    torch.cuda.synchronize()

@@ -94,7 +94,8 @@ def test_attention_refusals(lib):
     for name in ("plan", "table", "Q", "out", "ws"):
         assert _attend(lib, **{name: None}) == B.EINVAL, name
     for over in (dict(plan=A + 4), dict(Q=A + 8), dict(out=A + 2), dict(ws=A + 8), dict(q_stride=8 * 128 - 8), dict(out_stride=8 * 128 + 4), dict(scale=-1.0),
-                 dict(scale=float("nan")), dict(scale=float("inf")), dict(softcap=-1.0), dict(softcap=float("nan")), dict(ws_bytes=100)):
+                 dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2e37), dict(softcap=-1.0), dict(softcap=float("nan")), dict(softcap=2e37),
+                 dict(softcap=1e-38), dict(scale=1e10, softcap=1e-30), dict(ws_bytes=100)):
         assert _attend(lib, **over) == B.EINVAL, over
     for over in (dict(n_kv_heads=1, page_stride=16 * 128), dict(page_size=32, page_stride=2 * 32 * 128), dict(n_pages=11)):
         assert _attend(lib, None, cache(**over)) == B.EINVAL, over
