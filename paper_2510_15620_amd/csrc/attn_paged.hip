@@ -817,8 +817,8 @@ extern "C" int prism_op_attention_paged(const prism_page_shape *shape, const pri
   a.q_stride = q_stride; a.out_stride = out_stride; a.page_stride = cache->page_stride;
   a.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)hd);
   a.softcap = softcap;
-  const float log2e = 1.4426950408889634f;                    // the 16-bit kernels keep plain scores unscaled, modified ones in units of log 2
-  a.unit = cache->dtype == PRISM_DTYPE_FP32 ? log2e : softcap > 0.f || slopes ? 1.0f : a.scale * log2e;
+  const float log2e = 1.4426950408889634f;                    // the 16-bit kernels keep plain scores unscaled, all others are in units of log 2
+  a.unit = cache->dtype == PRISM_DTYPE_FP32 || softcap > 0.f || slopes ? 1.0f : a.scale * log2e;
   a.page_shift = __builtin_ctz(cache->page_size);
   hipStream_t s = (hipStream_t)stream;
   if (cache->dtype == PRISM_DTYPE_FP32) {

@@ -3,9 +3,11 @@
 // accumulators of S^T are the next contraction's operand.
 //
 // A workgroup of four waves takes 32 rows of an item.  Every wave has all of them, as two blocks of 16 that share a group of 16 keys in
-// registers, and every fourth group; the four meet in LDS.  What bounds it is the way from the L2 caches, since every wave fetches its
-// keys for itself: us of 40 ragged chunks over up to 900 keys, 4 heads of 64, with 16 rows per wave 76 (62 without either product), with
-// 32 70 (head size 128, where two blocks spill: 16 164, 32 285).
+// registers, and every fourth group; the four meet in LDS.  What bounds it: the products keep the matrix pipes busy
+// for 17 us of the 57 that 40 ragged chunks over up to 900 keys take, 4 heads of 64; the rest is the softmax's instructions (125 to 32
+// products of 16 rows and keys) and compute units with a long chunk more than others.  With 16 rows per wave instead of 32 it was 76
+// to 70; head size 128, where two blocks spill, 164 to 285.  Weights are powers of 2 of scores in units of log 2: the factor's rounding
+// is 2^-25 of a score, as much as the score's own, and expf's range steps and exact splitting cost 9 us.
 #include <type_traits>
 
 #include "paged.h"
@@ -98,6 +100,8 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       o[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   }
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float scale2 = a.scale * kLog2e;
   wait_loads<0>();                                            // the queries are here: nothing in the loop waits for them
   auto work = [&](auto block, int grp, int page, const f32x4 (&k)[NB], const Values &t) __attribute__((always_inline)) {
     constexpr int I = decltype(block)::value;
@@ -111,46 +115,64 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
         s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b][s], qf[I][b][s], s0, 0, 0, 0);
         s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b + 1][s], qf[I][b + 1][s], s1, 0, 0, 0);
       }
+    // scores in units of log 2
     const bool masked = page < 0 || k0 + 15 > b_first[I] || k0 + 15 >= limit || (window > 0 && k0 <= b_last[I] - window);
-    const int lo = window > 0 ? pos[I] - window + 1 : 0, hi = pos[I] < limit - 1 ? pos[I] : limit - 1;
-    float p[4], mx = -INFINITY;
-    bool see[4];
+    float p[4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int key = k0 + 4 * g + s;
-      p[s] = (s0[s] + s1[s]) * a.scale;
-      if (MOD) {
-        if (a.softcap > 0.f) p[s] = a.softcap * tanhf(p[s] / a.softcap);
-        p[s] -= slope[I] * (float)(pos[I] - key);
+    for (int s = 0; s < 4; ++s) p[s] = s0[s] + s1[s];
+    if (MOD) {
+      if (a.softcap > 0.f) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) p[s] = a.softcap * tanhf(p[s] * a.scale / a.softcap);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) p[s] *= a.scale;
       }
-      see[s] = !masked || (page >= 0 && key >= lo && key <= hi);
-      if (!see[s]) p[s] = -INFINITY;
-      mx = fmaxf(mx, p[s]);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) p[s] = (p[s] - slope[I] * (float)(pos[I] - (k0 + 4 * g + s))) * kLog2e;
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) p[s] *= scale2;
     }
-    mx = max_xor32(max_xor16(mx));
+    bool see[4] = {true, true, true, true}, odd = false;
+    float v[4][NB];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) v[s][b] = t.v[s][b];
+    if (masked) {
+      const int lo = window > 0 ? pos[I] - window + 1 : 0, hi = pos[I] < limit - 1 ? pos[I] : limit - 1;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int key = k0 + 4 * g + s;
+        see[s] = page >= 0 && key >= lo && key <= hi;
+        if (!see[s]) p[s] = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          // a weight of zero times a value that is not finite would reach the sum: values of keys that no row sees become zero
+          if (page < 0 || key >= limit) v[s][b] = 0.f;
+          odd = odd || !(fabsf(v[s][b]) < INFINITY);
+        }
+      }
+    }
+    const float mx = max_xor32(max_xor16(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3]))));
     const float m_new = fmaxf(m_run[I], mx), ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
-    const float alpha = expf(m_run[I] - ref);
+    const float alpha = __builtin_amdgcn_exp2f(m_run[I] - ref);
     m_run[I] = m_new;
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      p[s] = expf(p[s] - ref);
+      p[s] = __builtin_amdgcn_exp2f(p[s] - ref);
       sum += p[s];
     }
     l_run[I] = l_run[I] * alpha + sum;
+    // the running maxima usually settle after a few groups; opaque, or the compiler makes it an unconditional multiply again
+    unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);
+    asm volatile("" : "+s"(moved));
+    if (moved != 0) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) o[I][b] *= alpha;
-    float v[4][NB];
-    bool odd = false;
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        v[s][b] = t.v[s][b];
-        // a weight of zero times a value that is not finite would reach the sum: values of keys that no row sees become zero
-        if (masked && (page < 0 || k0 + 4 * g + s >= limit)) v[s][b] = 0.f;
-        odd = odd || !(fabsf(v[s][b]) < INFINITY);
-      }
+      for (int b = 0; b < NB; ++b) o[I][b] *= alpha;
+    }
     if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
       // those of keys that some rows see and others do not go to the rows that see them by indicators
 #pragma unroll 1
@@ -219,7 +241,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       f32x4 y;
 #pragma unroll
       for (int q = 0; q < 4; ++q) y[q] = o[i][(4 * j + q) % NB][(4 * j + q) / NB];
-      *reinterpret_cast<f32x4 *>(&lO[wave][c][NB * 4 * g + 4 * j]) = y;
+      *reinterpret_cast<f32x4 *>(&lO[wave][c][((NB * g + j) ^ swizzle(c)) * 4]) = y;
     }
     if (g == 0) lml[wave][c] = make_float2(m_run[i], l_tot);
     __syncthreads();
@@ -235,8 +257,8 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       for (int w = 0; w < W; ++w) {
         const float2 x = lml[w][r16];
         if (x.x == -INFINITY) continue;                      // a wave without keys has nothing
-        const float f = expf(x.x - ref);
-        const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][r16][d]);
+        const float f = __builtin_amdgcn_exp2f(x.x - ref);
+        const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][r16][(d / 4 ^ swizzle(r16)) * 4]);
         sum += f * x.y;
 #pragma unroll
         for (int q = 0; q < 4; ++q) y[q] += f * z[q];

@@ -18,9 +18,10 @@ namespace prism {
 static const int kPlanRows = 128;        // query rows of a block
 static const int kPlanTile = 64;         // keys of a tile
 static const int kPlanItems = 1024;      // items wanted over all KV heads: twice the two workgroups that each of 256 compute units holds
-static const int kPlanMinTiles = 4;      // tiles of an item at least, where that leaves fewer items than wanted
+// tiles of an item at least, where that leaves fewer items than wanted (us for chunks of 40 passages in fp32, 4 heads of 64, with 4, 8
+// for blocks of many rows: 57, 62; in 16 bits equal)
+static const int kPlanMinTiles = 4;
 static const int kPlanNarrow = 32;       // rows of a sequence whose keys are cut freely
-static const int kPlanMinWide = 8;       // the same for the others
 static const int kJoinRows = 8;          // query rows whose parts one workgroup joins
 static const int kPlanMagic = 0x70616765;
 static const int kGroupMax = kPlanRows;  // query heads per KV head

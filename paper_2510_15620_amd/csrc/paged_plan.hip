@@ -195,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
     const double x = ceil((double)all_tiles / goal);
     return x < least ? least : x > 1 << 30 ? 1 << 30 : (int)x;
   };
-  const int narrow = share(a.goal, kPlanMinTiles), wide = share(a.wide_goal, kPlanMinWide);
+  const int narrow = share(a.goal, kPlanMinTiles), wide = share(a.wide_goal, kPlanMinTiles);
   mine = {0, 0, 0};
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
