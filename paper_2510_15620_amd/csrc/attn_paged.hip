@@ -627,7 +627,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
   __syncthreads();
   odd = odd_waves[0] | odd_waves[1] | odd_waves[2] | odd_waves[3];
   const float l_tot = sum_xor32(l_run);
-  if (!active || r_first + c >= rows) return;
+  if (!active) return;
   // lane holds d = 32 t + 8 (e / 4) + 4 half + e % 4 of its row
   if (odd) {
     for (int kt = it.tile0; kt < kt_end; ++kt) {
@@ -652,7 +652,9 @@ void attention_paged_16_kernel(const PagedAttn a) {
   }
   if (it.part0 < 0) {
     const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
-    OT *op = (OT *)a.out + (int64_t)(it.row0 + tok) * a.out_stride + (int64_t)head * HD + half * 4;
+    // through LDS of the wave's own, so that a store is whole rows: stored from the accumulators, eight bytes of 32 rows at a time, 60
+    // passages of 100 to 500 tokens take 165 us instead of 153
+    OT *const mine = (wave < 2 ? lV0 : lV1) + (wave & 1) * 32 * HD;
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
@@ -660,9 +662,17 @@ void attention_paged_16_kernel(const PagedAttn a) {
         vec4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = round_to<OT>(o[t][q * 4 + e] * inv);
-        *reinterpret_cast<vec4 *>(op + t * 32 + q * 8) = v;
+        *reinterpret_cast<vec4 *>(mine + c * HD + ((t * 4 + q) ^ swizzle_k<HD>(c)) * 8 + half * 4) = v;
       }
-  } else {
+    const int64_t to = (int64_t)(it.row0 + tok) * a.out_stride + (int64_t)head * HD;
+#pragma unroll
+    for (int j = 0; j < 32 / RI; ++j) {
+      const int row = j * RI + lane / CH, d = lane % CH;
+      const int64_t row_to = (int64_t)(uint32_t)__shfl((int)(to & 0xFFFFFFFF), row, 64) | (int64_t)__shfl((int)(to >> 32), row, 64) << 32;
+      const vec8 v = *reinterpret_cast<const vec8 *>(mine + row * HD + (d ^ swizzle_k<HD>(row)) * 8);
+      if (r_first + row < rows) *reinterpret_cast<vec8 *>((OT *)a.out + row_to + d * 8) = v;
+    }
+  } else if (r_first + c < rows) {
     const int64_t at = (int64_t)(it.part0 + r_first + c) * nkv + kvh;
     float *op = a.part_O + at * HD + half * 4;
 #pragma unroll
