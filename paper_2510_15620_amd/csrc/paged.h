@@ -15,6 +15,8 @@ namespace prism {
 // 128 rows, so those are cut into runs of twice that, and only where they have half as many again.  So per KV head
 //   items <= plan_goal + blocks,   items of cut blocks < 2 plan_goal, their rows < 128 plan_goal,
 // which is what bounds a launch's grid and the room for partial results without the host knowing a length.
+// Sequences of more than kPlanNarrow rows come first in the list: their items take longest, and the others fill what is left at the end
+// (30 single tokens over up to 4000 keys and a chunk of 500 behind them, 32 query heads over 8: 52 us, in the sequences' order 65).
 static const int kPlanRows = 128;        // query rows of a block
 static const int kPlanTile = 64;         // keys of a tile
 static const int kPlanItems = 1024;      // items wanted over all KV heads: twice the two workgroups that each of 256 compute units holds
@@ -33,7 +35,9 @@ struct PlanHeader {
   int32_t pad[4];
 };
 static_assert(sizeof(PlanHeader) == 64, "one cache-line half");
-struct PlanSeq { int32_t row0, rows, cached, has, page0, n_parts, item0, part0, join0, pad[3]; };  // page0: rank of its first new page
+// page0: rank of its first new page; item0: its first item where those of all sequences follow each other, and item0 + shift in the list,
+// where the sequences of many rows come first
+struct PlanSeq { int32_t row0, rows, cached, has, page0, n_parts, item0, shift, part0, join0, pad[2]; };
 struct PlanItem { int32_t seq, row0, n_tok, pos0, tile0, tile1, part0, pad; };        // part0: first partial row, -1: the block is whole
 struct PlanJoin { int32_t row0, n_tok, part0, n_parts, step, pad[3]; };                 // part j of its rows: from part0 + j * step on
 

@@ -37,30 +37,42 @@ struct PlanArgs {
 // Sums that stop at 2^31 - 1: of terms that are not negative, in any grouping the same
 __device__ __forceinline__ int add_capped(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
 
-// sums over the workgroup's threads in front of this one, of three values at once; total: over all of them
-struct Sums { int a, b, c; };
-template <int WAVES>
-__device__ __forceinline__ Sums block_scan(Sums v, Sums *lds, Sums &total) {
+// Sum over this lane and those in front of it: within rows of 16 lanes, then each row's last one to the rows behind it.  By moves between
+// lanes within the vector unit: a step through LDS's crossbar takes some ten times as long, and every sum here is waited for
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_from(int x) {
+  return add_capped(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = add_from<0x111, 0xF>(x);                               // from 1, 2, 4 and 8 lanes in front
+  x = add_from<0x112, 0xF>(x);
+  x = add_from<0x114, 0xF>(x);
+  x = add_from<0x118, 0xF>(x);
+  x = add_from<0x142, 0xA>(x);                               // lanes 15 and 47 to the row behind them
+  return add_from<0x143, 0xC>(x);                            // lane 31 to the upper half
+}
+// sums over the workgroup's threads in front of this one, of N values at once; total: over all of them
+template <int N> struct Sums { int v[N]; };
+template <int WAVES, int N>
+__device__ __forceinline__ Sums<N> block_scan(Sums<N> s, int32_t (&lds)[4][WAVES], Sums<N> &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Sums<N> out;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int a = __shfl_up(v.a, o, 64), b = __shfl_up(v.b, o, 64), c = __shfl_up(v.c, o, 64);
-    if (lane >= o) { v.a = add_capped(v.a, a); v.b = add_capped(v.b, b); v.c = add_capped(v.c, c); }
-  }
-  if (lane == 63) lds[wave] = v;
-  v = {__shfl_up(v.a, 1, 64), __shfl_up(v.b, 1, 64), __shfl_up(v.c, 1, 64)};
-  if (lane == 0) v = {0, 0, 0};
-  __syncthreads();
-  Sums before = {0, 0, 0};
-  total = {0, 0, 0};
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const Sums t = lds[w];
-    if (w == wave) before = total;
-    total.a = add_capped(total.a, t.a); total.b = add_capped(total.b, t.b); total.c = add_capped(total.c, t.c);
+  for (int i = 0; i < N; ++i) {
+    const int x = wave_scan(s.v[i]);
+    if (lane == 63) lds[i][wave] = x;
+    out.v[i] = __builtin_amdgcn_update_dpp(0, x, 0x138, 0xF, 0xF, false);      // of the lane in front
+    total.v[i] = 0;
   }
   __syncthreads();
-  return {add_capped(v.a, before.a), add_capped(v.b, before.b), add_capped(v.c, before.c)};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      if (w == wave) out.v[i] = add_capped(out.v[i], total.v[i]);
+      total.v[i] = add_capped(total.v[i], lds[i][w]);
+    }
+  __syncthreads();
+  return out;
 }
 
 // the last i in [0, n) with first[i] <= x; first[0] = 0
@@ -129,7 +141,7 @@ __device__ __forceinline__ void lay_out(const PlanArgs &a, const int32_t *row0, 
       it.tile0 = lo;
       it.tile1 = lo + n;
     }
-    a.items[i] = it;
+    a.items[i + sq.shift] = it;
   }
 }
 
@@ -137,8 +149,7 @@ __device__ __forceinline__ void lay_out(const PlanArgs &a, const int32_t *row0, 
 template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
   constexpr bool kRecords = THREADS * PER <= kPlanInLds;     // the sequences' records in LDS too, for laying rows out
-  __shared__ Sums scan[THREADS / 64];
-  __shared__ int64_t tile_sums[THREADS / 64];
+  __shared__ __align__(16) int32_t scan[4][THREADS / 64];
   __shared__ int32_t row0[kRecords ? THREADS * PER : 1], item0[kRecords ? THREADS * PER : 1];
   __shared__ PlanSeq records[kRecords ? THREADS * PER : 1];
   const prism_page_shape &s = a.s;
@@ -147,21 +158,21 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
   int n_free = *a.n_free;
   n_free = n_free < 0 ? 0 : n_free > a.free_cap ? a.free_cap : n_free;
   int cached[PER], rows[PER], tiles[PER], has[PER], fresh_pages[PER], n_blocks[PER], n_parts[PER], r0[PER];
-  Sums total, mine = {0, 0, 0};
+  Sums<1> sum = {0}, run, total;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const bool in = first + k < s.n_seqs;
     const int c = in ? a.cached[first + k] : 0, f = in ? a.fresh[first + k] : 0;
     cached[k] = c < 0 ? 0 : c > (1 << 29) ? 1 << 29 : c;
     rows[k] = f < 0 ? 0 : f;
-    mine.a = add_capped(mine.a, rows[k]);
+    sum.v[0] = add_capped(sum.v[0], rows[k]);
   }
-  Sums run = block_scan<THREADS / 64>(mine, scan, total);
-  const int asked = total.a, done = asked < s.n_tokens ? asked : s.n_tokens;
+  run = block_scan<THREADS / 64>(sum, scan, total);
+  const int asked = total.v[0], done = asked < s.n_tokens ? asked : s.n_tokens;
   // rows behind the last of T are left out; pages, blocks and tiles of what is left
-  int at = run.a;
-  int64_t block_tiles = 0;
-  mine = {0, 0, 0};
+  int at = run.v[0];
+  int64_t block_tiles = 0;                                    // of up to four sequences: below 2^46
+  Sums<4> part = {{0, 0, 0, 0}}, parts;                       // new pages; the tiles, 16 bits at a time
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     r0[k] = at < s.n_tokens ? at : s.n_tokens;
@@ -179,41 +190,44 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
     }
     tiles[k] = t;
     block_tiles += (int64_t)t * n_blocks[k];
-    mine.a = add_capped(mine.a, fresh_pages[k]);
+    part.v[0] = add_capped(part.v[0], fresh_pages[k]);
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) block_tiles += __shfl_xor(block_tiles, o, 64);
-  if ((threadIdx.x & 63) == 0) tile_sums[threadIdx.x >> 6] = block_tiles;
-  run = block_scan<THREADS / 64>(mine, scan, total);
-  int page = run.a;
-  const int pages = total.a;
-  int64_t all_tiles = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) all_tiles += tile_sums[w];
+  for (int i = 0; i < 3; ++i) part.v[1 + i] = (int)(block_tiles >> (16 * i)) & 0xFFFF;
+  int page = block_scan<THREADS / 64>(part, scan, parts).v[0];
+  const int pages = parts.v[0];
+  const int64_t all_tiles = parts.v[1] + ((int64_t)parts.v[2] << 16) + ((int64_t)parts.v[3] << 32);
   // Tiles of an item, rounded up, so at least the quotient (exact below 2^53): what bounds the number of items
   auto share = [&](int goal, int least) {
     const double x = ceil((double)all_tiles / goal);
     return x < least ? least : x > 1 << 30 ? 1 << 30 : (int)x;
   };
   const int narrow = share(a.goal, kPlanMinTiles), wide = share(a.wide_goal, kPlanMinTiles);
-  mine = {0, 0, 0};
+  enum { kItems, kWide, kRows, kJoins };                     // items, those of them with many rows, partial rows, joins
+  Sums<4> mine = {{0, 0, 0, 0}}, all;
+  auto add = [&](Sums<4> &x, int k) {
+    const int items = n_blocks[k] * n_parts[k];
+    x.v[kItems] += items;
+    if (rows[k] * a.G > kPlanNarrow) x.v[kWide] += items;
+    if (n_parts[k] > 1) {
+      x.v[kRows] += rows[k] * a.G * n_parts[k];
+      x.v[kJoins] += a.join(rows[k] + jt - 1);
+    }
+  };
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const bool one = rows[k] * a.G <= kPlanNarrow;
     const int per_item = one ? narrow : wide;
     n_parts[k] = (one ? tiles[k] > narrow : tiles[k] > wide + wide / 2) ? (tiles[k] + per_item - 1) / per_item : 1;
-    mine.a += n_blocks[k] * n_parts[k];
-    if (n_parts[k] > 1) {
-      mine.b += rows[k] * a.G * n_parts[k];
-      mine.c += a.join(rows[k] + jt - 1);
-    }
+    add(mine, k);
   }
-  run = block_scan<THREADS / 64>(mine, scan, total);
+  Sums<4> front = block_scan<THREADS / 64>(mine, scan, all);
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int q = first + k;
     if (q >= s.n_seqs) break;
-    const PlanSeq o = {r0[k], rows[k], cached[k], has[k], page, n_parts[k], run.a, run.b, run.c, {0, 0, 0}};
+    const int shift = rows[k] * a.G > kPlanNarrow ? front.v[kWide] - front.v[kItems] : all.v[kWide] - front.v[kWide];
+    const PlanSeq o = {r0[k], rows[k], cached[k], has[k], page, n_parts[k], front.v[kItems], shift, front.v[kRows], front.v[kJoins], {0, 0}};
     a.seqs[q] = o;
     if (kRecords) {
       row0[q] = o.row0;
@@ -222,11 +236,7 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
     }
     a.cu[q] = o.row0;
     page = add_capped(page, fresh_pages[k]);
-    run.a += n_blocks[k] * n_parts[k];
-    if (n_parts[k] > 1) {
-      run.b += rows[k] * a.G * n_parts[k];
-      run.c += a.join(rows[k] + jt - 1);
-    }
+    add(front, k);
   }
   if (threadIdx.x == 0) {
     const int taken = pages < n_free ? pages : n_free;
@@ -241,15 +251,15 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
     PlanHeader o;
     o.magic = kPlanMagic;
     o.shape = s;
-    o.n_items = total.a;
-    o.n_joins = total.c;
+    o.n_items = all.v[kItems];
+    o.n_joins = all.v[kJoins];
     o.n_free = n_free;                                       // the caller's count may be overwritten before the rows are laid out
     for (int k = 0; k < 4; ++k) o.pad[k] = 0;
     *a.head = o;
   }
   if (!kRecords || s.n_tokens > kPlanAlone) return;
   __syncthreads();
-  lay_out(a, row0, item0, records, done, total.a, n_free, threadIdx.x, THREADS);
+  lay_out(a, row0, item0, records, done, all.v[kItems], n_free, threadIdx.x, THREADS);
 }
 
 __global__ __launch_bounds__(256) void page_rows_kernel(const PlanArgs a) {

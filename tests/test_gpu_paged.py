@@ -44,6 +44,8 @@ def _check_work(plan, cu, cached, page, width, G, nkv, window):
     items = raw[items_at: items_at + 8 * n_items].reshape(-1, 8)
     joins = raw[items_at + 8 * most:][: 8 * n_joins].reshape(-1, 8)
     room = min(goal * 128, plan.n_tokens * G * (goal + 1))
+    many = [(cu[seq + 1] - cu[seq]) * G > 32 for seq in items[:, 0].tolist()]
+    assert many == sorted(many, reverse=True), "sequences of many rows come first"
     seen, parts = {}, {}
     for seq, row0, n_tok, pos0, t0, t1, part, _ in items.tolist():
         assert 0 <= seq < n and 1 <= n_tok <= bt and cu[seq] <= row0 and row0 + n_tok <= cu[seq + 1] and (row0 - cu[seq]) % bt == 0
