@@ -152,9 +152,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
 
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
-  const PlanItem it = load_const(a.items + item);             // within the list's room, whatever it holds: asked for with the header
-  const PlanHeader plan = load_const(a.plan);
-  if (plan.magic != kPlanMagic || !same_shape(plan.shape, a.shape) || item >= plan.n_items) return;
+  PlanItem it;
+  if (!load_item(a, item, it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = it.n_tok * G, window = a.shape.window;
   const int cap_keys = a.shape.max_pages << a.page_shift;

@@ -27,9 +27,8 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   __shared__ float2 lml[W][16];
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
-  const PlanItem it = load_const(a.items + item);
-  const PlanHeader plan = load_const(a.plan);
-  if (plan.magic != kPlanMagic || !same_shape(plan.shape, a.shape) || item >= plan.n_items) return;
+  PlanItem it;
+  if (!load_item(a, item, it)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int rows = it.n_tok * G, row_begin = blockIdx.y * kRows, window = a.shape.window, cap_keys = a.shape.max_pages << a.page_shift;
   const int last = it.pos0 + it.n_tok - 1, limit = last + 1 < cap_keys ? last + 1 : cap_keys;

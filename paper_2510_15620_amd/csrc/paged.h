@@ -71,9 +71,10 @@ __host__ __device__ inline size_t plan_items_at(const prism_page_shape &s) { ret
 __host__ __device__ inline size_t plan_joins_at(const prism_page_shape &s) { return plan_items_at(s) + (size_t)plan_items(s) * sizeof(PlanItem); }
 __host__ __device__ inline size_t plan_bytes(const prism_page_shape &s) { return plan_joins_at(s) + (size_t)plan_joins(s) * sizeof(PlanJoin); }
 
+// without branches: on the device every one would be a wait of its own
 __host__ __device__ inline bool same_shape(const prism_page_shape &a, const prism_page_shape &b) {
-  return a.n_seqs == b.n_seqs && a.n_tokens == b.n_tokens && a.n_q_heads == b.n_q_heads && a.n_kv_heads == b.n_kv_heads &&
-         a.page_size == b.page_size && a.n_pages == b.n_pages && a.max_pages == b.max_pages && a.window == b.window;
+  return (a.n_seqs == b.n_seqs) & (a.n_tokens == b.n_tokens) & (a.n_q_heads == b.n_q_heads) & (a.n_kv_heads == b.n_kv_heads) &
+         (a.page_size == b.page_size) & (a.n_pages == b.n_pages) & (a.max_pages == b.max_pages) & (a.window == b.window);
 }
 int check_page_shape(const prism_page_shape *s, const char *who);
 int check_kv_cache(const prism_kv_cache *c, const char *who);
@@ -133,6 +134,16 @@ struct PagedAttn {
   float scale, softcap, unit;
   int page_shift;
 };
+// Item `item` of the plan into `it`; false: there is none, or the plan was made for another shape.  The header and the item, which lies
+// within the list's room whatever it holds, are asked for together: left to itself the compiler asks for one field after the other
+__device__ __forceinline__ bool load_item(const PagedAttn &a, int item, PlanItem &it) {
+  it = load_const(a.items + item);
+  const PlanHeader h = load_const(a.plan);
+  asm volatile("" : : "s"(it.seq), "s"(it.row0), "s"(it.n_tok), "s"(it.pos0), "s"(it.tile0), "s"(it.tile1), "s"(it.part0), "s"(h.magic),
+               "s"(h.shape.n_seqs), "s"(h.shape.n_tokens), "s"(h.shape.n_q_heads), "s"(h.shape.n_kv_heads), "s"(h.shape.page_size),
+               "s"(h.shape.n_pages), "s"(h.shape.max_pages), "s"(h.shape.window), "s"(h.n_items));
+  return (h.magic == kPlanMagic) & same_shape(h.shape, a.shape) & (item < h.n_items);
+}
 int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s);
 
 }  // namespace prism
