@@ -307,7 +307,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
                 pf[b][kb * 4 + e + 1] = ph[1];
               }
             l_run[b] = l_run[b] * alpha + psum;
-            unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);   // as below
+            // the running maxima usually settle after a few steps; opaque, or the compiler makes it an unconditional multiply again
+            unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);
             asm volatile("" : "+s"(moved));
             if (moved != 0) {
 #pragma unroll
@@ -448,7 +449,12 @@ void attention_paged_16_kernel(const PagedAttn a) {
   for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  // What the exponents are taken from: a row's largest score, but an old one until a new one is 2^3 times its weight.  With 32 rows some
+  // maximum moves in many tiles, and every move is a multiplication of all accumulators; weights of up to 2^3 cost nothing (half holds
+  // them times 2^12, so up to 2^15).  us with every new maximum taken and with this: chunks of 16 heads of 64 250, 238; of 32 heads of 128
+  // with a cap 636, 617, without 951, 949
+  const float slack = fminf(3.0f / c_exp, 1e30f);
+  float m_run = -INFINITY, m_move = -INFINITY, mb = -P16::kLift, l_run = 0.f;      // a score above m_move moves m_run; mb: what exponents lose
 
   // a wave stages the tile's keys 16 wave .. 16 wave + 15; all four groups' pages say which keys exist
   struct Entries { int e[4]; };
@@ -575,9 +581,19 @@ void attention_paged_16_kernel(const PagedAttn a) {
         for (int e = 0; e < 16; ++e) mxk[kb] = fmaxf(mxk[kb], s[kb][e]);
       __builtin_amdgcn_sched_barrier(0);
       const float mx = max_xor32(fmaxf(mxk[0], mxk[1]));
-      const float m_new = fmaxf(m_run, mx);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;     // no key yet: weights exp(-inf) = 0
-      const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c_exp), mb = ref * c_exp - P16::kLift;
+      if (__builtin_amdgcn_ballot_w64(mx > m_move) != 0) {
+        const float m_new = mx > m_move ? mx : m_run;
+        const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
+        const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c_exp);
+        m_run = m_new;
+        mb = ref * c_exp - P16::kLift;
+        m_move = fabsf(mb) < 65536.f ? m_new + slack : m_new;   // beyond that, exponents' own roundings may need half's room
+        l_run *= alpha;
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+      }
       float psum = 0.f;
       vec8 pf[4];
 #pragma unroll
@@ -591,17 +607,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
           pf[kb * 2 + (e >> 3)][e & 7] = ph[0];
           pf[kb * 2 + (e >> 3)][(e & 7) + 1] = ph[1];
         }
-      l_run = l_run * alpha + psum;
-      m_run = m_new;
-      // the running maxima usually settle after a few tiles; opaque, or the compiler makes it an unconditional multiply again
-      unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);
-      asm volatile("" : "+s"(moved));
-      if (moved != 0) {
-#pragma unroll
-        for (int t = 0; t < HD / 32; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
-      }
+      l_run += psum;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll

@@ -155,22 +155,20 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       }
     }
     const float mx = max_xor32(max_xor16(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3]))));
-    const float m_new = fmaxf(m_run[I], mx), ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
-    const float alpha = __builtin_amdgcn_exp2f(m_run[I] - ref);
-    m_run[I] = m_new;
-    float sum = 0.f;
+    // exponents are taken from an old maximum until a new one is 2^3 times its weight: as it moves the accumulators have to be multiplied
+    if (__builtin_amdgcn_ballot_w64(mx > m_run[I] + 3.0f) != 0) {
+      const float m_new = mx > m_run[I] + 3.0f ? mx : m_run[I];
+      const float alpha = __builtin_amdgcn_exp2f(m_run[I] - (m_new == -INFINITY ? 0.f : m_new));
+      m_run[I] = m_new;
+      l_run[I] *= alpha;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) o[I][b] *= alpha;
+    }
+    const float ref = m_run[I] == -INFINITY ? 0.f : m_run[I];  // no key yet: weights exp(-inf) = 0
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       p[s] = __builtin_amdgcn_exp2f(p[s] - ref);
-      sum += p[s];
-    }
-    l_run[I] = l_run[I] * alpha + sum;
-    // the running maxima usually settle after a few groups; opaque, or the compiler makes it an unconditional multiply again
-    unsigned long long moved = __builtin_amdgcn_ballot_w64(alpha != 1.0f);
-    asm volatile("" : "+s"(moved));
-    if (moved != 0) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) o[I][b] *= alpha;
+      l_run[I] += p[s];
     }
     if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
       // those of keys that some rows see and others do not go to the rows that see them by indicators

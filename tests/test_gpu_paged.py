@@ -439,6 +439,22 @@ def test_a_captured_step_replays_on_new_lengths():
             assert torch.equal(graphed[name], eager[name]), (k, name)
 
 
+@pytest.mark.parametrize("dtype,nq,hd", [(F16, 8, 128), (BF16, 14, 64), (F32, 8, 64)])
+@pytest.mark.parametrize("fresh", [1, 3, 90])
+@pytest.mark.parametrize("factor,rising", [(0.05, True), (30.0, False), (30.0, True), (3000.0, True)])
+def test_attention_of_small_and_large_scores_that_rise(dtype, nq, hd, fresh, factor, rising):
+    """Scores whose maxima stay close together, or rise from key to key by little or by much: what the exponents are taken from moves late,
+    once, or in every tile."""
+    s = R.Step([1500], [fresh], 64, nq, 2, hd, dtype, seed=5, stale=float("nan"))
+    s.make_plan()
+    up = torch.linspace(0.2, 1.0, 1500 + fresh).to(DEV) if rising else torch.ones(1500 + fresh, device=DEV)
+    pages = s.d_table[0].long()[torch.arange(1500 + fresh, device=DEV) // 64]
+    key = s.Q[0, :hd].float().abs() + 0.1
+    s.K[pages, :, torch.arange(1500 + fresh, device=DEV) % 64] = (up[:, None, None] * key).to(dtype).expand(-1, 2, -1)
+    s.Q.copy_((s.Q.float().abs() + 0.1).to(dtype))
+    s.check(factor / hd, 0.0, None)
+
+
 def test_same_inputs_same_bits():
     s = R.Step([9000, 30, 500], [1, 1, 70], 16, 8, 2, 128, BF16, seed=2)
     s.make_plan()
