@@ -5,8 +5,8 @@
 // four sequences per thread, three scans); what they say about each row and item is then independent work, found by a binary
 // search.  Steps of up to kPlanAlone rows are finished by the same workgroup, larger ones by a second launch of many.
 // Bound by launch and memory latency and by the chain of the sums, a step's bytes being nothing: 24 sequences of a token each 6.1 us, 500
-// of 332 tokens in the mean 13.6 us in two launches.  So there is no division but by shift
-// and multiplication, every wave's load of a value is asked for once, and 64 bits only where a sum needs them.
+// of 332 tokens in the mean 11.5 us in two launches.  So there is no division but by shift and multiplication, every wave's load of a
+// value is asked for once, and 64 bits only where a sum needs them.
 #include "paged.h"
 
 namespace prism {
@@ -322,8 +322,12 @@ extern "C" int prism_op_page_plan(const prism_page_shape *shape, const int32_t *
   a.goal = plan_goal(*shape);
   a.wide_goal = plan_wide_goal(*shape);
   hipStream_t s = (hipStream_t)stream;
-  // few sequences and rows: as many waves as have something to do, since every barrier waits for all of them
-  if (shape->n_seqs <= 256 && shape->n_tokens <= 1024) page_plan_kernel<256, 1><<<1, 256, 0, s>>>(a);
+  // Every barrier waits for all waves, so few of them where they only sum: us with four waves and with sixteen, 4 sequences 7.6, 10.2, 60
+  // 9.0, 11.5, 500 11.5, 13.6, 900 13.9, 15.1; more than that 20.7, 18.2 (1500).  Where the workgroup lays the rows out too, sixteen from 1024 rows on
+  const bool alone = shape->n_tokens <= kPlanAlone;
+  if (shape->n_seqs <= 256 && (shape->n_tokens <= 1024 || !alone)) page_plan_kernel<256, 1><<<1, 256, 0, s>>>(a);
+  else if (shape->n_seqs <= 512 && !alone) page_plan_kernel<256, 2><<<1, 256, 0, s>>>(a);
+  else if (shape->n_seqs <= kPlanInLds && !alone) page_plan_kernel<256, 4><<<1, 256, 0, s>>>(a);
   else if (shape->n_seqs <= kPlanInLds) page_plan_kernel<1024, 1><<<1, 1024, 0, s>>>(a);
   else page_plan_kernel<1024, PRISM_MAX_CANDS / 1024><<<1, 1024, 0, s>>>(a);
   PRISM_HIP(hipGetLastError());

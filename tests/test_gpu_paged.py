@@ -88,7 +88,8 @@ def _lengths(r, n, c_hi, f_hi):
 
 @pytest.mark.parametrize("n,c_hi,f_hi,page,pad,nq,nkv,window", [
     (1, 0, 1, 16, 0, 8, 2, 0), (3, 40, 20, 16, 5, 8, 8, 0), (70, 900, 3, 32, 0, 32, 8, 0), (300, 200, 40, 64, 100, 14, 2, 100),
-    (1500, 60, 9, 256, 3, 3, 1, 17), (4096, 33, 2, 16, 0, 32, 8, 0), (2, 9000, 6000, 128, 1, 71, 1, 0), (40, 100, 400, 16, 0, 6, 2, 64)])
+    (1500, 60, 9, 256, 3, 3, 1, 17), (256, 500, 90, 16, 0, 32, 8, 0), (257, 500, 90, 16, 7, 14, 2, 64), (513, 70, 40, 64, 0, 8, 1, 0), (1024, 50, 30, 16, 2, 8, 2, 0),
+    (4096, 33, 2, 16, 0, 32, 8, 0), (2, 9000, 6000, 128, 1, 71, 1, 0), (40, 100, 400, 16, 0, 6, 2, 64)])
 def test_plan_of_ragged_steps(n, c_hi, f_hi, page, pad, nq, nkv, window):
     r = np.random.default_rng(n + page)
     c, f = _lengths(r, n, c_hi, f_hi)
