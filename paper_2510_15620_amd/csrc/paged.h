@@ -60,6 +60,13 @@ __host__ __device__ inline int64_t plan_joins(const prism_page_shape &s) {
   const int64_t by_tokens = s.n_tokens / t + s.n_seqs, by_blocks = (int64_t)plan_goal(s) * (plan_block_tokens(s) / t);
   return by_tokens < by_blocks ? by_tokens : by_blocks;    // fewer than goal blocks are cut
 }
+// tiles that a block's window can touch, and those of the longest sequence: where they are too few for a cut, there is nothing to join
+__host__ __device__ inline int64_t plan_window_tiles(const prism_page_shape &s) {
+  return ((int64_t)s.window + plan_block_tokens(s) + kPlanTile - 2) / kPlanTile + 1;
+}
+inline bool plan_may_cut(const prism_page_shape &s) {
+  return ((int64_t)s.max_pages * s.page_size + kPlanTile - 1) / kPlanTile > kPlanMinTiles && (s.window == 0 || plan_window_tiles(s) > kPlanMinTiles);
+}
 // Partial rows of a KV head.  Of the tiles, w in wide blocks and n in narrow ones, w + n = 1: fewer than 2 n goal parts of up to
 // kPlanNarrow rows and w goal of up to kPlanRows, so goal kPlanRows at most; and every row is in goal + 1 parts at most.
 __host__ __device__ inline int64_t plan_part_rows(const prism_page_shape &s) {

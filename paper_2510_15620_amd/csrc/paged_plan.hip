@@ -32,7 +32,7 @@ struct PlanArgs {
   PlanItem *items;
   PlanJoin *joins;
   Divisor block, join;                    // by the tokens of a block and of a join
-  int free_cap, page_shift, G, goal, wide_goal;
+  int free_cap, page_shift, G, goal, wide_goal, window_tiles;
 };
 
 // Sums that stop at 2^31 - 1: of terms that are not negative, in any grouping the same
@@ -156,6 +156,7 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
   const prism_page_shape &s = a.s;
   const int first = threadIdx.x * PER, bt = a.block.d, jt = a.join.d, psize = 1 << a.page_shift, cap = s.max_pages << a.page_shift;
 
+  const int window_tiles = a.window_tiles;
   int n_free = *a.n_free;
   n_free = n_free < 0 ? 0 : n_free > a.free_cap ? a.free_cap : n_free;
   int cached[PER], rows[PER], tiles[PER], has[PER], fresh_pages[PER], n_blocks[PER], n_parts[PER], r0[PER];
@@ -185,10 +186,7 @@ __global__ __launch_bounds__(THREADS) void page_plan_kernel(const PlanArgs a) {
     fresh_pages[k] = rows[k] > 0 ? (np < s.max_pages ? np : s.max_pages) - has[k] : 0;
     n_blocks[k] = a.block(rows[k] + bt - 1);
     int t = ((end < cap ? end : cap) + kPlanTile - 1) / kPlanTile;
-    if (s.window > 0) {                                      // tiles that a block's window can touch
-      const int w = (int)(((int64_t)s.window + bt + kPlanTile - 2) / kPlanTile) + 1;
-      t = t < w ? t : w;
-    }
+    t = t < window_tiles ? t : window_tiles;
     tiles[k] = t;
     block_tiles += (int64_t)t * n_blocks[k];
     part.v[0] = add_capped(part.v[0], fresh_pages[k]);
@@ -321,6 +319,7 @@ extern "C" int prism_op_page_plan(const prism_page_shape *shape, const int32_t *
   a.G = shape->n_q_heads / shape->n_kv_heads;
   a.goal = plan_goal(*shape);
   a.wide_goal = plan_wide_goal(*shape);
+  a.window_tiles = shape->window > 0 ? (int)plan_window_tiles(*shape) : INT32_MAX;
   hipStream_t s = (hipStream_t)stream;
   // Every barrier waits for all waves, so few of them where they only sum: us with four waves and with sixteen, 4 sequences 7.6, 10.2, 60
   // 9.0, 11.5, 500 11.5, 13.6, 900 13.9, 15.1; more than that 20.7, 18.2 (1500).  Where the workgroup lays the rows out too, sixteen from 1024 rows on

@@ -223,6 +223,18 @@ def test_attention_over_split_keys(dtype, nq, nkv, hd, cached, fresh):
     s.check()
 
 
+@pytest.mark.parametrize("dtype,nq,nkv,hd", [(F16, 8, 8, 128), (BF16, 4, 1, 64), (F32, 2, 2, 64)])
+@pytest.mark.parametrize("cached,fresh,width,window", [([255, 200, 100, 0], [1, 1, 40, 256], 16, 0), ([256, 200], [1, 72], 17, 0), ([9000, 255, 50], [1, 1, 90], None, 65),
+                                                       ([9000, 255, 50], [1, 1, 90], None, 66), ([9000, 700], [1, 200], None, 200)])
+def test_attention_around_the_fewest_tiles_that_are_cut(dtype, nq, nkv, hd, cached, fresh, width, window):
+    """Caches and windows of four tiles are never cut, and their results are written without a joining launch; of five they may be."""
+    s = R.Step(cached, fresh, 16, nq, nkv, hd, dtype, seed=11, window=window, width=width, stale=float("nan"))
+    s.make_plan()
+    tiles = min(s.table.shape[1] * 16 / 64, (window + 128 // (nq // nkv) + 62) // 64 + 1 if window else 1e9)
+    assert tiles > 4 or int(s.plan.buffer[:64].view(torch.int32)[10]) == 0
+    s.check()
+
+
 @pytest.mark.parametrize("dtype,nq,nkv,hd", [(F16, 16, 8, 128), (BF16, 14, 2, 64), (F32, 6, 2, 64)])
 @pytest.mark.parametrize("window,softcap,with_slopes,scale", [(1, 0.0, False, 0.0), (50, 0.0, False, 0.0), (64, 5.0, False, 0.3), (0, 30.0, True, 0.0),
                                                               (200, 0.0, True, 0.0), (5000, 2.0, True, 1.0)])
