@@ -189,8 +189,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
     __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[0]), PRISM_LDS_PTR(dst), 16, 0, 0);
     __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[1]), PRISM_LDS_PTR(dst), 16, 1024, 0);
     if constexpr (NI == 4) {
-      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[2]), PRISM_LDS_PTR(dst), 16, 2048, 0);
-      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[3]), PRISM_LDS_PTR(dst), 16, 3072, 0);
+      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[2]), PRISM_LDS_PTR(dst), 16, 2 * 1024, 0);
+      __builtin_amdgcn_global_load_lds(PRISM_GLOBAL_PTR(s + o[3]), PRISM_LDS_PTR(dst), 16, 3 * 1024, 0);
     }
   };
 
