@@ -135,6 +135,10 @@ struct Modifier {
   __device__ __forceinline__ float bias(int key) const { return __builtin_fmaf(slope, (float)key, rest); }
 };
 
+// Exponents are s c - mb, an instruction a score, with mb the maximum's product.  Beyond kFar mb's rounding shows in the weights (2^-8 there, and
+// from 2^27 on they would leave half's range), so the maximum is subtracted from the scores first.
+static constexpr float kFar = 65536.f;
+
 // Two workgroups on a compute unit where the registers of three do not hold all (MOD, HD 64, chunks of 14 heads over a window of 1000:
 // 55 us, with three and 18 values kept in memory 64)
 template <typename OT, int HD, bool MOD>
@@ -294,7 +298,13 @@ void attention_paged_16_kernel(const PagedAttn a) {
             mx = max_xor32(max_xor16(mx));
             const float m_new = fmaxf(m_run[b], mx);
             const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
-            const float alpha = __builtin_amdgcn_exp2f((m_run[b] - ref) * c_exp), mb = ref * c_exp - P16::kLift;
+            const float alpha = __builtin_amdgcn_exp2f((m_run[b] - ref) * c_exp);
+            float mb = ref * c_exp - P16::kLift;
+            if (__builtin_amdgcn_ballot_w64(!(fabsf(mb) < kFar)) != 0) {
+              mb = -P16::kLift;
+#pragma unroll
+              for (int kb = 0; kb < 2; ++kb) s[b][kb] -= ref;
+            }
             m_run[b] = m_new;
             float psum = 0.f;
 #pragma unroll
@@ -457,6 +467,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
   // with a cap 636, 617, without 951, 949
   const float slack = fminf(3.0f / c_exp, 1e30f);
   float m_run = -INFINITY, m_move = -INFINITY, mb = -P16::kLift, l_run = 0.f;      // a score above m_move moves m_run; mb: what exponents lose
+  unsigned long long far = 0;                                 // some row's mb is beyond kFar
 
   // a wave stages the tile's keys 16 wave .. 16 wave + 15; all four groups' pages say which keys exist
   struct Entries { int e[4]; };
@@ -589,12 +600,22 @@ void attention_paged_16_kernel(const PagedAttn a) {
         const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c_exp);
         m_run = m_new;
         mb = ref * c_exp - P16::kLift;
-        m_move = fabsf(mb) < 65536.f ? m_new + slack : m_new;   // beyond that, exponents' own roundings may need half's room
+        far = __builtin_amdgcn_ballot_w64(!(fabsf(mb) < kFar));
+        m_move = fabsf(mb) < kFar ? m_new + slack : m_new;
         l_run *= alpha;
 #pragma unroll
         for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+      }
+      float mb_tile = mb;
+      if (far != 0) {
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        mb_tile = -P16::kLift;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kb][e] -= ref;
       }
       float psum = 0.f;
       vec8 pf[4];
@@ -603,8 +624,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           typename P16::vec2 ph;
-          ph[0] = (OT)__builtin_amdgcn_exp2f(s[kb][e] * c_exp - mb);
-          ph[1] = (OT)__builtin_amdgcn_exp2f(s[kb][e + 1] * c_exp - mb);
+          ph[0] = (OT)__builtin_amdgcn_exp2f(s[kb][e] * c_exp - mb_tile);
+          ph[1] = (OT)__builtin_amdgcn_exp2f(s[kb][e + 1] * c_exp - mb_tile);
           psum = P16::sum2(ph, psum);
           pf[kb * 2 + (e >> 3)][e & 7] = ph[0];
           pf[kb * 2 + (e >> 3)][(e & 7) + 1] = ph[1];

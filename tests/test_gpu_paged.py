@@ -468,6 +468,32 @@ def test_attention_of_small_and_large_scores_that_rise(dtype, nq, hd, fresh, fac
     s.check(factor / hd, 0.0, None)
 
 
+@pytest.mark.parametrize("dtype,nq,hd", [(F16, 8, 128), (BF16, 14, 64), (F32, 8, 64)])
+@pytest.mark.parametrize("fresh", [1, 3, 90])
+@pytest.mark.parametrize("power", [6, 12, 20, 24])
+def test_attention_of_far_scores(dtype, nq, hd, fresh, power):
+    """Scores far from zero and from each other: the keys with the largest share all the weight equally."""
+    n = 700 + fresh
+    s = R.Step([700], [fresh], 64, nq, 2, hd, dtype, seed=6, stale=float("nan"))
+    s.make_plan()
+    pages, at = s.d_table[0].long()[torch.arange(n, device=DEV) // 64], torch.arange(n, device=DEV) % 64
+    size = 2.0 ** (min(power, 14) if dtype is F16 else power)
+    k = torch.zeros(n, hd, device=DEV)
+    k[:, 0] = torch.arange(n, device=DEV) % 3 * size                          # 0, 1 and 2 times: every third key has the largest score
+    s.K[pages, :, at] = k.to(dtype)[:, None].expand(-1, 2, -1)
+    s.Q.zero_()
+    s.Q[:, ::hd] = 2.0 ** (min(power, 15) if dtype is F16 else power)
+    out = s.attend()
+    top = torch.arange(n, device=DEV) % 3 == 2
+    for h in range(nq):
+        v = s.V[pages, h // (nq // 2), at].double()
+        for i in range(fresh):
+            seen = top & (torch.arange(n, device=DEV) <= 700 + i)
+            want = v[seen].mean(0)
+            step = 2 * R.HALF_STEP[dtype] * want.abs() + n * 2.0 ** -24 * v.abs().max()     # its rounding, and the sums'
+            assert ((out[i, h * hd:(h + 1) * hd].double() - want).abs() <= step).all()
+
+
 def test_same_inputs_same_bits():
     s = R.Step([9000, 30, 500], [1, 1, 70], 16, 8, 2, 128, BF16, seed=2)
     s.make_plan()
