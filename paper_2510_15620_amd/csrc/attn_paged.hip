@@ -467,7 +467,6 @@ void attention_paged_16_kernel(const PagedAttn a) {
   // with a cap 636, 617, without 951, 949
   const float slack = fminf(3.0f / c_exp, 1e30f);
   float m_run = -INFINITY, m_move = -INFINITY, mb = -P16::kLift, l_run = 0.f;      // a score above m_move moves m_run; mb: what exponents lose
-  unsigned long long far = 0;                                 // some row's mb is beyond kFar
 
   // a wave stages the tile's keys 16 wave .. 16 wave + 15; all four groups' pages say which keys exist
   struct Entries { int e[4]; };
@@ -595,27 +594,25 @@ void attention_paged_16_kernel(const PagedAttn a) {
       __builtin_amdgcn_sched_barrier(0);
       const float mx = max_xor32(fmaxf(mxk[0], mxk[1]));
       if (__builtin_amdgcn_ballot_w64(mx > m_move) != 0) {
-        const float m_new = mx > m_move ? mx : m_run;
+        const float m_new = mx > m_move ? fmaxf(mx, m_run) : m_run;
         const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key yet: weights exp(-inf) = 0
         const float alpha = __builtin_amdgcn_exp2f((m_run - ref) * c_exp);
         m_run = m_new;
+        m_move = m_new + slack;
         mb = ref * c_exp - P16::kLift;
-        far = __builtin_amdgcn_ballot_w64(!(fabsf(mb) < kFar));
-        m_move = fabsf(mb) < kFar ? m_new + slack : m_new;
         l_run *= alpha;
 #pragma unroll
         for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
-      }
-      float mb_tile = mb;
-      if (far != 0) {
-        const float ref = m_run == -INFINITY ? 0.f : m_run;
-        mb_tile = -P16::kLift;
+        if (__builtin_amdgcn_ballot_w64(!(fabsf(mb) < kFar)) != 0) {
+          mb = -P16::kLift;
+          m_move = -INFINITY;                                 // here again in the next tile, and in all that have a key
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+          for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[kb][e] -= ref;
+            for (int e = 0; e < 16; ++e) s[kb][e] -= ref;
+        }
       }
       float psum = 0.f;
       vec8 pf[4];
@@ -624,8 +621,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
           typename P16::vec2 ph;
-          ph[0] = (OT)__builtin_amdgcn_exp2f(s[kb][e] * c_exp - mb_tile);
-          ph[1] = (OT)__builtin_amdgcn_exp2f(s[kb][e + 1] * c_exp - mb_tile);
+          ph[0] = (OT)__builtin_amdgcn_exp2f(s[kb][e] * c_exp - mb);
+          ph[1] = (OT)__builtin_amdgcn_exp2f(s[kb][e + 1] * c_exp - mb);
           psum = P16::sum2(ph, psum);
           pf[kb * 2 + (e >> 3)][e & 7] = ph[0];
           pf[kb * 2 + (e >> 3)][(e & 7) + 1] = ph[1];

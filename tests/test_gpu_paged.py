@@ -494,6 +494,17 @@ def test_attention_of_far_scores(dtype, nq, hd, fresh, power):
             assert ((out[i, h * hd:(h + 1) * hd].double() - want).abs() <= step).all()
 
 
+@pytest.mark.parametrize("dtype,nq,hd", [(F16, 8, 128), (BF16, 14, 64), (F32, 8, 64)])
+@pytest.mark.parametrize("cached,fresh,window", [([500], [90], 0), ([500], [90], 100), ([3, 500], [70, 3], 0), ([9000], [40], 0)])
+def test_attention_of_far_rows_beside_near_ones(dtype, nq, hd, cached, fresh, window):
+    """One head of a group has scores of some 2^17, the others of a few; eight keys of a page have twice the others'."""
+    s = R.Step(cached, fresh, 16, nq, 2, hd, dtype, seed=8, window=window, stale=float("nan"))
+    s.make_plan()
+    s.Q[:, :hd] *= 4096.0
+    s.K[:, :, : 8] *= 2.0
+    s.check()
+
+
 def test_same_inputs_same_bits():
     s = R.Step([9000, 30, 500], [1, 1, 70], 16, 8, 2, 128, BF16, seed=2)
     s.make_plan()
