@@ -751,7 +751,7 @@ __global__ __launch_bounds__(2 * HD) void paged_join_kernel(const PagedAttn a) {
         v *= f0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (x[u].x == -INFINITY) continue;                    // a part without keys has nothing
+          if (x[u].x == -INFINITY && x[u].y == 0.f) continue;   // a part without keys has nothing; one whose scores all are NaN has that maximum too
           const float f = __builtin_amdgcn_exp2f((x[u].x - ref) * a.unit);
           sum += f * x[u].y;
 #pragma unroll
@@ -770,7 +770,7 @@ __global__ __launch_bounds__(2 * HD) void paged_join_kernel(const PagedAttn a) {
         f32x4 w = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < deal; ++j) {
           const float2 x = lml[first + j];
-          if (x.x == -INFINITY) continue;
+          if (x.x == -INFINITY && x.y == 0.f) continue;
           const float f = __builtin_amdgcn_exp2f((x.x - ref) * a.unit);
           const f32x4 y = *reinterpret_cast<const f32x4 *>(&lO[first + j][d]);
           total += f * x.y;

@@ -253,7 +253,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
 #pragma unroll
       for (int w = 0; w < W; ++w) {
         const float2 x = lml[w][r16];
-        if (x.x == -INFINITY) continue;                      // a wave without keys has nothing
+        if (x.x == -INFINITY && x.y == 0.f) continue;        // a wave without keys has nothing; one whose scores all are NaN has that maximum too
         const float f = __builtin_amdgcn_exp2f(x.x - ref);
         const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][r16][(d / 4 ^ swizzle(r16)) * 4]);
         sum += f * x.y;
