@@ -106,27 +106,54 @@ template <typename OT> __device__ __forceinline__ float infinite_only(OT v) {
   return fabsf(x) < INFINITY ? 0.f : x;
 }
 
-// Scores with a cap, slopes or both, in units of log 2: (cap tanh(s scale / cap) - slope (p - k)) log2(e).  With tanh(u) = 1 - 2 / (1 + e^2u),
-// good to some 1e-7 absolutely (less than the rounding of the scores' operands), a score is one of
-//   -2 cap / (1 + 2^(in s)) + (slope k + rest),   in s + (slope k + rest)
-// where the factors hold scale and log2(e), k counts from the tile's first key of the lane and rest has cap, slope and the row's position.
+// Scores with a cap, slopes or both, in units of log 2: (cap tanh(u) - slope (p - k)) log2(e), u = s scale / cap.
+//   caps up to kExactCap: with tanh(u) = 1 - 2 / (1 + e^2u) a score is -2 cap / (1 + 2^(in s)) + (slope k + rest), off by 2^-22 of the cap, at most
+//     2^-16, where the weights' own rounding is 2^-12 or more;
+//   larger caps: that would be as large as the scores themselves.  Where |u| <= 1/2, (in s) (tanh(u) / u) + (slope k + rest) with a polynomial of
+//     u^2, off by 2^-23 of the score; beyond, tanh as above, 2^-22 of a cap that the score is no longer small against.
+// The factors hold scale and log2(e), k counts from the tile's first key of the lane and rest has slope, the row's position and the first form's cap.
 struct Modifier {
-  float in, minus_two_cap, slope, rest;
-  bool capped;
-  __device__ __forceinline__ Modifier(float scale, float cap, float slope_, int away) {
-    constexpr float kLog2e = 1.4426950408889634f;
-    capped = cap > 0.f;
-    in = capped ? scale * (2.0f * kLog2e) / cap : scale * kLog2e;
-    minus_two_cap = -2.0f * cap * kLog2e;
+  static constexpr float kLog2e = 1.4426950408889634f, kExactCap = 64.f;
+  float in, small, cap, slope, rest;                          // small: from s to u
+  bool capped, large;
+  __device__ __forceinline__ Modifier(float scale, float softcap, float slope_, int away) {
+    capped = softcap > 0.f;
+    large = softcap > kExactCap;
+    small = capped ? scale / softcap : 0.f;
+    in = capped && !large ? scale * (2.0f * kLog2e) / softcap : scale * kLog2e;
+    cap = softcap * kLog2e;
     slope = slope_ * kLog2e;
-    rest = (capped ? cap * kLog2e : 0.f) - slope * (float)away;
+    rest = (capped && !large ? cap : 0.f) - slope * (float)away;
+  }
+  // tanh(u) / u for u^2 = z <= 1/4: of the polynomials of degree 4 that are 1 at 0 the one whose largest relative error is smallest (2^-26)
+  static __device__ __forceinline__ float ratio(float z) {
+    return __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(0.017241491f, z, -0.0530454926f), z, 0.13325879f), z, -0.333331436f), z, 1.0f);
   }
   // Scores s[i] of the keys key(i), i < N.  One branch around all of them: with one around each none of the exponentials and
-  // reciprocals overlap (32 heads of 128, a cap, 7000 tokens over 2000 to 4000 more: 752 and 631 us)
+  // reciprocals overlap (32 heads of 128, a cap, 7000 tokens over 2000 to 4000 more: 752 and 631 us).  With the polynomial for caps of 50 too
+  // they take 622 instead of 599, and where scores reach the cap 881
   template <int N, typename S, typename Key> __device__ __forceinline__ void operator()(S &s, Key key) const {
-    if (capped) {
+    if (large) {
+      float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(minus_two_cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[i] * in)), bias(key(i)));
+      for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(s[i]));
+      if (__builtin_amdgcn_ballot_w64(most * small > 0.5f) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float u = s[i] * small;
+          s[i] = __builtin_fmaf(s[i] * in, ratio(u * u), bias(key(i)));
+        }
+      } else {                                                // each by its size: small ones beside one that reaches minus the cap have all the weight
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float u = s[i] * small;
+          const float far = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * (2.0f * kLog2e))), cap);
+          s[i] = (fabsf(u) <= 0.5f ? s[i] * in * ratio(u * u) : far) + bias(key(i));
+        }
+      }
+    } else if (capped) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[i] * in)), bias(key(i)));
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) s[i] = __builtin_fmaf(s[i], in, bias(key(i)));
