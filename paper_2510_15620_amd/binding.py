@@ -400,6 +400,13 @@ def _ints(t, n: int, device: int, what: str) -> int:
     raise PrismError(EINVAL, f"{what}: a dense int32 tensor of {n} values on the current device")
 
 
+def _table(t, plan, device: int) -> int:
+    """Address of a page table: rows of plan.max_pages entries, or a flat tensor of them."""
+    if t.dim() > 1 and t.shape[-1] != plan.max_pages:
+        raise PrismError(EINVAL, f"table: rows of {t.shape[-1]} pages for a plan of {plan.max_pages}")
+    return _ints(t, plan.n_seqs * plan.max_pages, device, "table")
+
+
 def _rows(t, dtype, device: int, what: str):
     """Address, row stride, rows and width of a two-dimensional device tensor whose rows are dense."""
     if t.dim() == 2 and t.dtype is dtype and t.get_device() == device:
@@ -473,7 +480,7 @@ def op_page_plan(plan: PagePlan, cached, fresh, table, free_pages, n_free, n_fre
     if plan.device != d:
         raise PrismError(EINVAL, "op_page_plan: the plan is on another device than the current one")
     _check(lib().prism_op_page_plan(
-        plan._ref, _ints(cached, n, d, "cached"), _ints(fresh, n, d, "fresh"), _ints(table, n * plan.max_pages, d, "table"),
+        plan._ref, _ints(cached, n, d, "cached"), _ints(fresh, n, d, "fresh"), _table(table, plan, d),
         _ints(free_pages, 0, d, "free_pages"), free_pages.numel(), _ints(n_free, 1, d, "n_free"), _ints(n_free_left, 1, d, "n_free_left"),
         _ints(cu, n + 1, d, "cu"), _ints(pos, T, d, "pos"), _ints(slot, T, d, "slot"),
         0 if status is None else _ints(status, 4, d, "status"), plan.buffer.data_ptr(), stream))
@@ -516,5 +523,5 @@ def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace,
     if slopes is not None and (slopes.dtype is not _torch.float32 or slopes.numel() != plan.n_q_heads or not slopes.is_contiguous() or slopes.get_device() != d):
         raise PrismError(EINVAL, "op_attention_paged: slopes of n_q_heads fp32 values")
     _check(lib().prism_op_attention_paged(
-        plan._ref, cache._ref, plan.buffer.data_ptr(), _ints(table, plan.n_seqs * plan.max_pages, d, "table"), q, q_stride, scale, softcap,
+        plan._ref, cache._ref, plan.buffer.data_ptr(), _table(table, plan, d), q, q_stride, scale, softcap,
         0 if slopes is None else slopes.data_ptr(), o, o_stride, workspace.data_ptr(), workspace.nbytes, stream))
