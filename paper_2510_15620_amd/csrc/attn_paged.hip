@@ -716,6 +716,10 @@ void attention_paged_16_kernel(const PagedAttn a) {
         for (int e = 0; e < 4; ++e) v[e] = round_to<OT>(o[t][q * 4 + e] * inv);
         *reinterpret_cast<vec4 *>(mine + c * HD + ((t * 4 + q) ^ swizzle_k<HD>(c)) * 8 + half * 4) = v;
       }
+    // (LDS serves a wave in order; the fences keep the compiler to it, the barrier, no instruction, makes the lanes meet)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     const int64_t to = (int64_t)(it.row0 + tok) * a.out_stride + (int64_t)head * HD;
 #pragma unroll
     for (int j = 0; j < 32 / RI; ++j) {
