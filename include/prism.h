@@ -365,6 +365,8 @@ int prism_op_qkv_finish_paged(const prism_kv_cache *cache, int32_t qkv_dtype, co
  * (scale, softcap and scale / softcap below 1e37),
  * softmax over the keys seen, times V.  A query that sees no key gives zeros; rows behind the last sequence are not written.  Keys
  * and values that a query does not see never reach its result, whatever they hold (NaN and infinities included).
+ * Of what it does see, a score that is NaN makes the row NaN, and a value that is not finite is the result in its dimension whatever its
+ * weight (infinities of both signs: NaN).  Results of type F16 saturate at its largest finite numbers.
  *   shape, plan, table: those of prism_op_page_plan (with a plan of another shape nothing is written).  Q, out: n_tokens rows of
  *   n_q_heads * head_dim values of the cache's type, q_stride / out_stride apart (rows 16-byte aligned); out may be Q itself.
  *   slopes [n_q_heads] fp32 [device] or NULL.

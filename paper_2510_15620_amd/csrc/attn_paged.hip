@@ -91,7 +91,7 @@ __device__ __forceinline__ u32x4 clean_fragment(u32x4 v, u32x4 keep, u16x2 &wors
   return v;
 }
 template <typename OT> __device__ __forceinline__ bool not_finite(u16x2 worst) { return worst[0] >= Paged16<OT>::kExp || worst[1] >= Paged16<OT>::kExp; }
-// Of keys that some rows see and others do not, the finite values go through the matrix cores ...
+// Of keys that some rows see and others do not, the finite values go through the matrix cores, and the others where they are seen, at the end
 template <typename OT> __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -99,11 +99,6 @@ template <typename OT> __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
     if ((v[w] >> 16 & Paged16<OT>::kExp) == Paged16<OT>::kExp) v[w] &= 0xFFFFu;
   }
   return v;
-}
-// ... and the others are added where they are seen, at the end: a weight above zero times one of them is that value
-template <typename OT> __device__ __forceinline__ float infinite_only(OT v) {
-  const float x = to_f32(v);
-  return fabsf(x) < INFINITY ? 0.f : x;
 }
 
 // Scores with a cap, slopes or both, in units of log 2: (cap tanh(u) - slope (p - k)) log2(e), u = s scale / cap.
@@ -394,26 +389,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
             for (int b = 0; b < RB; ++b) o[b][t] = P16::mma16(vf[t], pf[b], o[b][t]);
         }
       }
-      if (odd) {
-        for (int i = (it.tile0 * 2 + wave) * 2; i < s_end * 2; i += i & 1 ? 7 : 1) {     // both halves of each of this wave's steps
-          const int k0 = i * 16, page = page_of(k0);
-          if (page < 0 || !(mixed(k0 & ~31) || page_of(k0 & ~31) < 0 || page_of(k0 | 16) < 0)) continue;
-          const OT *v = Vh + rows_at(page, k0) + g * 4;
-          for (int key = k0; key < k0 + 16 && key < limit; ++key, v += HD) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-              if (key > pos[b] || (window > 0 && key <= pos[b] - window)) continue;
-#pragma unroll
-              for (int t = 0; t < HD / 16; ++t) {
-                const vec4 x = *reinterpret_cast<const vec4 *>(v + t * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[b][t][e] += infinite_only<OT>(x[e]);
-              }
-            }
-          }
-        }
-      }
-      // ---- the four waves' results meet: values in lK0 / lK1 (two waves each), maxima and sums in lV0; 16 rows at a time
+      // ---- the four waves' results meet: values in lK0 / lK1 (two waves each), maxima and sums in lV0, a sum's sign says `odd`; 16 rows at a time
       float *const mine = reinterpret_cast<float *>(wave < 2 ? lK0 : lK1) + (wave & 1) * 16 * HD;
       float2 *const ml = reinterpret_cast<float2 *>(lV0);
 #pragma unroll
@@ -422,7 +398,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
         for (int t = 0; t < HD / 16; ++t) *reinterpret_cast<f32x4 *>(mine + c * HD + ((t * 4 + g) ^ c) * 4) = o[b][t];
         const float l = sum_xor32(sum_xor16(l_run[b]));
-        if (g == 0) ml[wave * 16 + c] = make_float2(m_run[b], l);
+        if (g == 0) ml[wave * 16 + c] = make_float2(m_run[b], odd ? -l : l);
         __syncthreads();
         const int r = tid / CH, d = tid % CH;                // row of the 16, eight of its dimensions
         const int row = b * 16 + r;
@@ -431,13 +407,15 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
           for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 16 + r].x);
           const float ref = m == -INFINITY ? 0.f : m;
+          unsigned signs = 0;
           float sum = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const float2 x = ml[w * 16 + r];
             const float f = __builtin_amdgcn_exp2f((x.x - ref) * c_exp);
             const float *src = reinterpret_cast<const float *>(w < 2 ? lK0 : lK1) + (w & 1) * 16 * HD + r * HD;
-            sum += f * x.y;
+            sum += f * fabsf(x.y);
+            signs |= __float_as_uint(x.y);
             if (x.x != -INFINITY) {                          // a wave without keys has nothing (and its zero weight is none)
 #pragma unroll
               for (int q = 0; q < 2; ++q) {
@@ -448,6 +426,16 @@ void attention_paged_16_kernel(const PagedAttn a) {
             }
           }
           const int t = row / G, h = kvh * G + row - t * G;
+          float most = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) most = worst_of(v[e], most);
+          if (((signs >> 31) | !(most < INFINITY)) && sum == sum) {
+            float s[8];
+            sum_not_finite<OT, HD>(a, table, Vh + d * 8, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
+                                   window > 0 ? it.pos0 + t - window + 1 : 0, it.pos0 + t, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = s[e] == 0.f ? v[e] : s[e];
+          }
           if (it.part0 < 0) {
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
             vec8 y;
@@ -532,8 +520,8 @@ void attention_paged_16_kernel(const PagedAttn a) {
     return k0 + 63 > first || k0 + 63 >= limit || (window > 0 && k0 <= last - window);
   };
   // A tile in which some rows of the block do not see some keys: a weight of zero times a value that is not finite would reach the sum.
-  // So before the others read it, a wave clears what it staged of keys that nobody sees, and of the other keys what is not finite; those
-  // values are added where they are seen, at the end (`odd`).
+  // So before the others read it, a wave clears what it staged of keys that nobody sees, and of the other keys what is not finite; rows
+  // that see those values get them at the end (`odd`).
   bool odd = false;
   auto clean = [&](int kt, int page, auto buf_tag) __attribute__((always_inline)) {
     OT *const v = (decltype(buf_tag)::value ? lV1 : lV0) + wave * 16 * HD + lane * 8;
@@ -681,26 +669,26 @@ void attention_paged_16_kernel(const PagedAttn a) {
   const float l_tot = sum_xor32(l_run);
   if (!active) return;
   // lane holds d = 32 t + 8 (e / 4) + 4 half + e % 4 of its row
-  if (odd) {
-    for (int kt = it.tile0; kt < kt_end; ++kt) {
-      if (pages_from(entries_of(kt), kt).there == 15u && !mixed(kt * 64, it.pos0, last)) continue;
-      for (int k0 = kt * 64; k0 < kt * 64 + 64 && k0 < limit; k0 += 16) {
-        const int page = page_of(k0);
-        if (page < 0) continue;
-        const OT *v = Vh + rows_at(page, k0) + half * 4;
-        for (int key = k0; key < k0 + 16 && key < limit; ++key, v += HD) {
-          if (key > pos || (window > 0 && key <= pos - window)) continue;
+  float most = 0.f;
 #pragma unroll
-          for (int t = 0; t < HD / 32; ++t)
+  for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const vec4 x = *reinterpret_cast<const vec4 *>(v + t * 32 + q * 8);
+    for (int e = 0; e < 16; ++e) most = worst_of(o[t][e], most);
+  if (odd || __builtin_amdgcn_ballot_w64(!(most < INFINITY) && l_tot == l_tot) != 0) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[t][q * 4 + e] += infinite_only<OT>(x[e]);
-            }
-        }
+    for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        most = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = worst_of(o[t][q * 4 + e], most);
+        if (!odd && __builtin_amdgcn_ballot_w64(!(most < INFINITY)) == 0) continue;
+        float s[4];
+        sum_not_finite<OT, HD>(a, table, Vh + t * 32 + q * 8 + half * 4, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
+                               window > 0 ? pos - window + 1 : 0, pos, s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t][q * 4 + e] = s[e] == 0.f ? o[t][q * 4 + e] : s[e];
       }
-    }
   }
   if (it.part0 < 0) {
     const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
@@ -779,14 +767,14 @@ __global__ __launch_bounds__(2 * HD) void paged_join_kernel(const PagedAttn a) {
         const float f0 = __builtin_amdgcn_exp2f((m - ref) * a.unit);
         m = mx;
         sum *= f0;
-        v *= f0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (x[u].x == -INFINITY && x[u].y == 0.f) continue;   // a part without keys has nothing; one whose scores all are NaN has that maximum too
+        for (int e = 0; e < 4; ++e) v[e] = weighed(f0, v[e]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {                           // (a part without keys has zeros, one in the place of none weighs nothing)
           const float f = __builtin_amdgcn_exp2f((x[u].x - ref) * a.unit);
           sum += f * x[u].y;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] += f * y[u][e];
+          for (int e = 0; e < 4; ++e) v[e] += weighed(f, y[u][e]);
         }
       }
       *reinterpret_cast<f32x4 *>(&lO[group][d]) = v;
@@ -801,12 +789,11 @@ __global__ __launch_bounds__(2 * HD) void paged_join_kernel(const PagedAttn a) {
         f32x4 w = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < deal; ++j) {
           const float2 x = lml[first + j];
-          if (x.x == -INFINITY && x.y == 0.f) continue;
           const float f = __builtin_amdgcn_exp2f((x.x - ref) * a.unit);
           const f32x4 y = *reinterpret_cast<const f32x4 *>(&lO[first + j][d]);
           total += f * x.y;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] += f * y[e];
+          for (int e = 0; e < 4; ++e) w[e] += weighed(f, y[e]);
         }
         const int t = row / G, h = kvh * G + row - t * G;
         Out o;

@@ -24,7 +24,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   constexpr int W = 4, kRows = fp32_rows(NB);                 // waves; rows of a workgroup
   constexpr int CH = HD / 4, RI = 64 / CH, NI = 16 / RI;      // 16-byte chunks of a row; rows of a load instruction, instructions for 16 rows
   __shared__ __align__(16) float lO[W][16][HD];               // a wave's 16 keys, at the end its results
-  __shared__ float2 lml[W][16];
+  __shared__ float2 lml[W][16];                               // maxima and sums; a sum's sign says `found`
   const int nkv = a.shape.n_kv_heads, G = a.shape.n_q_heads / nkv;
   const int kvh = blockIdx.x % nkv, item = blockIdx.x / nkv;
   PlanItem it;
@@ -82,6 +82,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
   const bool both = RB > 1 && row_begin + 16 < rows;
   int pos[RB], b_first[RB], b_last[RB];                       // b_first, b_last: positions of a block's first and last row
   float slope[RB], m_run[RB], l_run[RB];
+  bool found = false;                                         // values that are not finite were kept from the products
   f32x4 qf[RB][NB], o[RB][NB];
 #pragma unroll
   for (int i = 0; i < RB; ++i) {
@@ -171,23 +172,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       l_run[I] += p[s];
     }
     if (masked && __builtin_amdgcn_ballot_w64(odd) != 0) {
-      // those of keys that some rows see and others do not go to the rows that see them by indicators
-#pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind) {
-        const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          f32x4 n = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            const float x = v[s][b];
-            const bool is = kind == 2 ? x != x : x == add;
-            n = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.0f : 0.0f, see[s] ? 1.0f : 0.0f, n, 0, 0, 0);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[I][b][e] += n[e] > 0.f ? add : 0.f;
-        }
-      }
+      found = true;                                           // rows that see those of keys that others do not see get them at the end
 #pragma unroll
       for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -240,7 +225,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       for (int q = 0; q < 4; ++q) y[q] = o[i][(4 * j + q) % NB][(4 * j + q) / NB];
       *reinterpret_cast<f32x4 *>(&lO[wave][c][((NB * g + j) ^ swizzle(c)) * 4]) = y;
     }
-    if (g == 0) lml[wave][c] = make_float2(m_run[i], l_tot);
+    if (g == 0) lml[wave][c] = make_float2(m_run[i], found ? -l_tot : l_tot);
     __syncthreads();
     for (int e = threadIdx.x; e < 16 * HD / 4; e += 64 * W) {
       const int r16 = e / (HD / 4), d = e % (HD / 4) * 4, row = row_begin + i * 16 + r16;
@@ -249,18 +234,29 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
 #pragma unroll
       for (int w = 0; w < W; ++w) m = fmaxf(m, lml[w][r16].x);
       const float ref = m == -INFINITY ? 0.f : m;
+      unsigned signs = 0;
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < W; ++w) {
         const float2 x = lml[w][r16];
-        if (x.x == -INFINITY && x.y == 0.f) continue;        // a wave without keys has nothing; one whose scores all are NaN has that maximum too
         const float f = __builtin_amdgcn_exp2f(x.x - ref);
         const f32x4 z = *reinterpret_cast<const f32x4 *>(&lO[w][r16][(d / 4 ^ swizzle(r16)) * 4]);
-        sum += f * x.y;
+        sum += f * fabsf(x.y);
+        signs |= __float_as_uint(x.y);
 #pragma unroll
         for (int q = 0; q < 4; ++q) y[q] += f * z[q];
       }
       const int t = row / G, h = kvh * G + row - t * G;
+      float most = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) most = worst_of(y[q], most);
+      if (((signs >> 31) | !(most < INFINITY)) && sum == sum) {
+        float s[4];
+        sum_not_finite<float, HD>(a, table, Vh + d, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit, window > 0 ? it.pos0 + t - window + 1 : 0,
+                                  it.pos0 + t, s);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = s[q] == 0.f ? y[q] : s[q];
+      }
       if (it.part0 < 0) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) y[q] = sum == 0.f ? 0.f : y[q] / sum;

@@ -151,6 +151,38 @@ __device__ __forceinline__ bool load_item(const PagedAttn &a, int item, PlanItem
                "s"(h.shape.n_pages), "s"(h.shape.max_pages), "s"(h.shape.window), "s"(h.n_items));
   return (h.magic == kPlanMagic) & same_shape(h.shape, a.shape) & (item < h.n_items);
 }
+// max(|x|, most), NaN if one of them is
+__device__ __forceinline__ float worst_of(float x, float most) { return __builtin_elementwise_maximum(__builtin_fabsf(x), most); }
+// Sum of what is not finite among a row's values of keys k_begin .. k_end - 1 (k_begin a multiple of 16) in N dimensions from V on, V a KV head's
+// place in the pool: 0 where all that the row sees, first .. pos, is finite.  A seen value that is not finite is the result, whatever its weight: in
+// the products its weight may underflow, at once or later with the maximum, and zero times it is NaN.  So wherever a result is not finite, or such values
+// were kept from rows that do not see them, they are looked up again here, at the price of reading V once more.  Ends early where all is NaN.
+template <typename T, int HD, int N>
+__device__ __forceinline__ void sum_not_finite(const PagedAttn &a, const int32_t *table, const T *V, int k_begin, int k_end, int first, int pos, float (&sum)[N]) {
+  struct alignas(N * sizeof(T)) Row { T v[N]; };
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.f;
+  for (int k0 = k_begin; k0 < k_end; k0 += 16) {
+    const int page = load_const(table + (k0 >> a.page_shift));
+    if ((unsigned)page >= (unsigned)a.shape.n_pages) continue;
+    const T *v = V + (int64_t)page * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
+    for (int key = k0; key < k0 + 16 && key < k_end; ++key, v += HD) {
+      const Row x = *reinterpret_cast<const Row *>(v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float f = to_f32(x.v[e]);
+        sum[e] += key >= first && key <= pos && !(fabsf(f) < INFINITY) ? f : 0.f;
+      }
+    }
+    bool open = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) open = open || sum[e] == sum[e];
+    if (__builtin_amdgcn_ballot_w64(open) == 0) return;
+  }
+}
+// Weight times a partial result, which stands whatever the weight where it is not finite
+__device__ __forceinline__ float weighed(float f, float y) { return fabsf(y) < INFINITY ? f * y : y; }
+
 int launch_attention_paged_fp32(const PagedAttn &a, int hd, hipStream_t s);
 
 }  // namespace prism
