@@ -370,6 +370,7 @@ int prism_op_qkv_finish_paged(const prism_kv_cache *cache, int32_t qkv_dtype, co
  *   shape, plan, table: those of prism_op_page_plan (with a plan of another shape nothing is written).  Q, out: n_tokens rows of
  *   n_q_heads * head_dim values of the cache's type, q_stride / out_stride apart (rows 16-byte aligned); out may be Q itself.
  *   slopes [n_q_heads] fp32 [device] or NULL.
+ *   A step of more than 2^24 workgroups is refused: one for each KV head and 64 to 128 rows of (token, query head) of a sequence, some 10^9 such rows.
  *   workspace [device], 16-byte aligned, prism_attention_paged_workspace bytes (-1 for a bad shape): partial results of queries whose
  *   keys are split over several workgroups.  Contents need no initialisation; calls that overlap need one each.
  * The order of a row's sums depends on the shape and on all lengths of the step, not on timing: same inputs, same bits. */

@@ -861,7 +861,9 @@ extern "C" int prism_op_attention_paged(const prism_page_shape *shape, const pri
   PRISM_REQUIRE(q_stride >= row && out_stride >= row && q_stride % vec == 0 && out_stride % vec == 0 &&
                 ((uintptr_t)plan | (uintptr_t)Q | (uintptr_t)out | (uintptr_t)workspace) % 16 == 0, PRISM_EINVAL,
                 "attention_paged: rows shorter than their heads, or not 16-byte aligned");
-  PRISM_REQUIRE(plan_items(*shape) * shape->n_kv_heads < (int64_t)1 << 31, PRISM_EINVAL, "attention_paged: too many work items");
+  // (a launch has fewer than 2^32 threads along its first axis)
+  PRISM_REQUIRE(plan_items(*shape) * shape->n_kv_heads < (int64_t)1 << 24, PRISM_EUNSUPPORTED, "attention_paged: too many work items (%lld over %d KV heads)",
+                (long long)plan_items(*shape), shape->n_kv_heads);
   PagedAttn a;
   a.shape = *shape;
   a.plan = (const PlanHeader *)plan;
