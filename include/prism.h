@@ -332,8 +332,8 @@ typedef struct {
 } prism_page_shape;
 
 /* Layout of a step, from the sequences' lengths.  cached, fresh [n_seqs]: tokens of each sequence in the cache before the step, and
- * tokens that the step brings (negative ones count as 0); its rows are sequence by sequence, row cu[s] + i at position
- * cached[s] + i.  All pointers [device].
+ * tokens that the step brings (negative ones count as 0, more than 2^29 cached ones, behind every table's end, as 2^29); its rows are
+ * sequence by sequence, row cu[s] + i at position cached[s] + i.  All pointers [device].
  *   table [n_seqs][max_pages], in and out: entries from ceil(cached / page_size) on that the step reaches get new pages, in order of
  *     sequence, then position, off the end of free_pages[0 .. *n_free) (at most free_cap entries); the others are not written.
  *     *n_free_left = free pages left; it may be n_free itself.  An entry for which there is no page left becomes -1.
