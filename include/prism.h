@@ -367,6 +367,8 @@ int prism_op_qkv_finish_paged(const prism_kv_cache *cache, int32_t qkv_dtype, co
  * and values that a query does not see never reach its result, whatever they hold (NaN and infinities included).
  * Of what it does see, a score that is NaN makes the row NaN, and a value that is not finite is the result in its dimension whatever its
  * weight (infinities of both signs: NaN).  Results of type F16 saturate at its largest finite numbers.
+ * Sums are fp32.  Weights are fp32 for dtype FP32; for the others they are rounded to that type before they meet V, 11 significant bits for F16,
+ * for BF16 8, in blocks of up to 32 rows of (token, query head) of a KV head, such as a single token's, 16 (prism_op_attention: 11 for both).
  *   shape, plan, table: those of prism_op_page_plan (with a plan of another shape nothing is written).  Q, out: n_tokens rows of
  *   n_q_heads * head_dim values of the cache's type, q_stride / out_stride apart (rows 16-byte aligned); out may be Q itself.
  *   slopes [n_q_heads] fp32 [device] or NULL.

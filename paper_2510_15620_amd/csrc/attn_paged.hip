@@ -6,7 +6,10 @@
 // its token.  As in attn_16.hip everything is computed transposed, S^T = K Q^T and O^T += V^T P^T, so that a lane owns one row and
 // the accumulators of S^T are the second contraction's operand as they are.  K and V lie in the cache as they are projected, a row
 // per key; V^T's fragments come out of LDS by the transposing read (ds_read_b64_tr_b16), so that appending a token is a row's store.
-// P is rounded to the type of V and the denominators sum the rounded weights.
+// P is rounded to the type of V, which the matrix cores ask for, and the denominators sum the rounded weights: 11 bits in half, as in
+// attn_16.hip, 8 in bf16, whose values half cannot hold.  Items of up to 32 rows, which wait for memory, take a bf16 weight as two numbers, the
+// second product with V costing nothing (100 sequences 315 us, 8.95 to 9.2 for three short ones); of more rows one, for there it would cost a fifth
+// (us: 32 heads of 128 with a cap 596 and 756, two chunks of 300 to 500 tokens 100 and 123, 60 passages 153 and 180).
 //
 // Two ways of dividing an item between its workgroup's four waves:
 //   more than 32 rows (chunks; bound by the power that matrix and vector work draw): 32 rows per wave, tiles of 64 keys shared through
@@ -30,6 +33,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 
 template <typename T> struct Paged16;
 template <> struct Paged16<bf16> {
+  static constexpr bool kTwoParts = true;                      // weights of items of few rows: two numbers
   static constexpr float kLift = 0.f;
   static constexpr unsigned kExp = 0x7F80u;
   typedef bf16x2 vec2;
@@ -37,6 +41,7 @@ template <> struct Paged16<bf16> {
   static __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Paged16<f16> {
+  static constexpr bool kTwoParts = false;
   static constexpr float kLift = 12.f;                         // weights are held times 2^12 (most 1): their small ones stay normal numbers
   static constexpr unsigned kExp = 0x7C00u;
   typedef __attribute__((ext_vector_type(2))) _Float16 vec2;
@@ -103,7 +108,7 @@ template <typename OT> __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
 
 // Scores with a cap, slopes or both, in units of log 2: (cap tanh(u) - slope (p - k)) log2(e), u = s scale / cap.
 //   caps up to kExactCap: with tanh(u) = 1 - 2 / (1 + e^2u) a score is -2 cap / (1 + 2^(in s)) + (slope k + rest), off by 2^-22 of the cap, at most
-//     2^-16, where the weights' own rounding is 2^-12 or more;
+//     2^-16, no more than what the weights lose to their own rounding;
 //   larger caps: that would be as large as the scores themselves.  Where |u| <= 1/2, (in s) (tanh(u) / u) + (slope k + rest) with a polynomial of
 //     u^2, off by 2^-23 of the score; beyond, tanh as above, 2^-22 of a cap that the score is no longer small against.
 // The factors hold scale and log2(e), k counts from the tile's first key of the lane and rest has slope, the row's position and the first form's cap.
@@ -293,7 +298,7 @@ void attention_paged_16_kernel(const PagedAttn a) {
               for (int kk = 0; kk < HD / 32; ++kk) s[b][kb] = P16::mma16(kf[2 * kk + kb], qf[b][kk], s[b][kb]);
             }
           const bool masked = cur0 < 0 || cur1 < 0 || mixed(k0);
-          vec8 pf[RB];
+          vec8 pf[RB], rest[P16::kTwoParts ? RB : 1];           // weights, and what their rounding left
 #pragma unroll
           for (int b = 0; b < RB; ++b) {
             if (MOD) {
@@ -333,12 +338,17 @@ void attention_paged_16_kernel(const PagedAttn a) {
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
               for (int e = 0; e < 4; e += 2) {
-                typename P16::vec2 ph;
-                ph[0] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e] * c_exp - mb);
-                ph[1] = (OT)__builtin_amdgcn_exp2f(s[b][kb][e + 1] * c_exp - mb);
+                const float p0 = __builtin_amdgcn_exp2f(s[b][kb][e] * c_exp - mb), p1 = __builtin_amdgcn_exp2f(s[b][kb][e + 1] * c_exp - mb);
+                const typename P16::vec2 ph = {(OT)p0, (OT)p1};
                 psum = P16::sum2(ph, psum);
                 pf[b][kb * 4 + e] = ph[0];
                 pf[b][kb * 4 + e + 1] = ph[1];
+                if constexpr (P16::kTwoParts) {
+                  const typename P16::vec2 pr = {(OT)(p0 - to_f32(ph[0])), (OT)(p1 - to_f32(ph[1]))};
+                  psum = P16::sum2(pr, psum);
+                  rest[b][kb * 4 + e] = pr[0];
+                  rest[b][kb * 4 + e + 1] = pr[1];
+                }
               }
             l_run[b] = l_run[b] * alpha + psum;
             // the running maxima usually settle after a few steps; opaque, or the compiler makes it an unconditional multiply again
@@ -386,7 +396,10 @@ void attention_paged_16_kernel(const PagedAttn a) {
 #pragma unroll
           for (int t = 0; t < HD / 16; ++t)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) o[b][t] = P16::mma16(vf[t], pf[b], o[b][t]);
+            for (int b = 0; b < RB; ++b) {
+              o[b][t] = P16::mma16(vf[t], pf[b], o[b][t]);
+              if constexpr (P16::kTwoParts) o[b][t] = P16::mma16(vf[t], rest[b], o[b][t]);
+            }
         }
       }
       // ---- the four waves' results meet: values in lK0 / lK1 (two waves each), maxima and sums in lV0, a sum's sign says `odd`; 16 rows at a time
