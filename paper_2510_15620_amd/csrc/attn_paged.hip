@@ -442,13 +442,9 @@ void attention_paged_16_kernel(const PagedAttn a) {
           float most = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) most = worst_of(v[e], most);
-          if (((signs >> 31) | !(most < INFINITY)) && sum == sum) {
-            float s[8];
-            sum_not_finite<OT, HD>(a, table, Vh + d * 8, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
-                                   window > 0 ? it.pos0 + t - window + 1 : 0, it.pos0 + t, s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = s[e] == 0.f ? v[e] : s[e];
-          }
+          if ((signs >> 31 || most != most) && sum == sum)
+            settle<OT, HD>(a, table, Vh + d * 8, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
+                           window > 0 ? it.pos0 + t - window + 1 : 0, it.pos0 + t, signs >> 31, v);
           if (it.part0 < 0) {
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
             vec8 y;
@@ -687,20 +683,17 @@ void attention_paged_16_kernel(const PagedAttn a) {
   for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) most = worst_of(o[t][e], most);
-  if (odd || __builtin_amdgcn_ballot_w64(!(most < INFINITY) && l_tot == l_tot) != 0) {
+  if (odd || __builtin_amdgcn_ballot_w64(most != most && l_tot == l_tot) != 0) {
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        most = 0.f;
+        float y[4] = {o[t][q * 4], o[t][q * 4 + 1], o[t][q * 4 + 2], o[t][q * 4 + 3]};
+        if (!odd && __builtin_amdgcn_ballot_w64(y[0] != y[0] || y[1] != y[1] || y[2] != y[2] || y[3] != y[3]) == 0) continue;
+        settle<OT, HD>(a, table, Vh + t * 32 + q * 8 + half * 4, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
+                       window > 0 ? pos - window + 1 : 0, pos, odd, y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most = worst_of(o[t][q * 4 + e], most);
-        if (!odd && __builtin_amdgcn_ballot_w64(!(most < INFINITY)) == 0) continue;
-        float s[4];
-        sum_not_finite<OT, HD>(a, table, Vh + t * 32 + q * 8 + half * 4, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
-                               window > 0 ? pos - window + 1 : 0, pos, s);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][q * 4 + e] = s[e] == 0.f ? o[t][q * 4 + e] : s[e];
+        for (int e = 0; e < 4; ++e) o[t][q * 4 + e] = y[e];
       }
   }
   if (it.part0 < 0) {

@@ -250,12 +250,11 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       float most = 0.f;
 #pragma unroll
       for (int q = 0; q < 4; ++q) most = worst_of(y[q], most);
-      if (((signs >> 31) | !(most < INFINITY)) && sum == sum) {
-        float s[4];
-        sum_not_finite<float, HD>(a, table, Vh + d, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit, window > 0 ? it.pos0 + t - window + 1 : 0,
-                                  it.pos0 + t, s);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = s[q] == 0.f ? y[q] : s[q];
+      if ((signs >> 31 || most != most) && sum == sum) {
+        float w[4] = {y[0], y[1], y[2], y[3]};
+        settle<float, HD>(a, table, Vh + d, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit, window > 0 ? it.pos0 + t - window + 1 : 0,
+                          it.pos0 + t, signs >> 31, w);
+        y = f32x4{w[0], w[1], w[2], w[3]};
       }
       if (it.part0 < 0) {
 #pragma unroll

@@ -153,32 +153,41 @@ __device__ __forceinline__ bool load_item(const PagedAttn &a, int item, PlanItem
 }
 // max(|x|, most), NaN if one of them is
 __device__ __forceinline__ float worst_of(float x, float most) { return __builtin_elementwise_maximum(__builtin_fabsf(x), most); }
-// Sum of what is not finite among a row's values of keys k_begin .. k_end - 1 (k_begin a multiple of 16) in N dimensions from V on, V a KV head's
-// place in the pool: 0 where all that the row sees, first .. pos, is finite.  A seen value that is not finite is the result, whatever its weight: in
-// the products its weight may underflow, at once or later with the maximum, and zero times it is NaN.  So wherever a result is not finite, or such values
-// were kept from rows that do not see them, they are looked up again here, at the price of reading V once more.  Ends early where all is NaN.
+// y: a row's sums of weights and values in N dimensions, V the place of its KV head in the pool from these on, keys k_begin .. k_end - 1 (k_begin a
+// multiple of 16), of which it sees first .. pos.  A seen value that is not finite is the result, whatever its weight: in the products the weight may
+// underflow, at once or later with the maximum, and zero times the value is NaN.  So where a sum is NaN, or such values were kept from rows that do
+// not see them (`all`), what is not finite is looked up again here and its sum taken instead, if there is any.  That is V read once more, until all
+// that is open is known to be NaN (in bf16 also where an infinity meets a weight's two parts): a token of 100 sequences over up to 8000 keys each,
+// with an infinity in every one, 1.4 ms instead of 0.32; with a NaN among the first keys no more than without.
 template <typename T, int HD, int N>
-__device__ __forceinline__ void sum_not_finite(const PagedAttn &a, const int32_t *table, const T *V, int k_begin, int k_end, int first, int pos, float (&sum)[N]) {
+__device__ __forceinline__ void settle(const PagedAttn &a, const int32_t *table, const T *V, int k_begin, int k_end, int first, int pos, bool all, float (&y)[N]) {
+  constexpr int U = 8;                                        // rows under way together
   struct alignas(N * sizeof(T)) Row { T v[N]; };
+  float sum[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) sum[e] = 0.f;
-  for (int k0 = k_begin; k0 < k_end; k0 += 16) {
+  for (int k0 = k_begin; k0 < k_end; k0 += U) {
     const int page = load_const(table + (k0 >> a.page_shift));
     if ((unsigned)page >= (unsigned)a.shape.n_pages) continue;
     const T *v = V + (int64_t)page * a.page_stride + (int64_t)(k0 & ((1 << a.page_shift) - 1)) * HD;
-    for (int key = k0; key < k0 + 16 && key < k_end; ++key, v += HD) {
-      const Row x = *reinterpret_cast<const Row *>(v);
+    Row x[U];
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float f = to_f32(x.v[e]);
-        sum[e] += key >= first && key <= pos && !(fabsf(f) < INFINITY) ? f : 0.f;
-      }
-    }
+    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const Row *>(v + u * HD);     // (of the same page, behind the last key too)
     bool open = false;
 #pragma unroll
-    for (int e = 0; e < N; ++e) open = open || sum[e] == sum[e];
-    if (__builtin_amdgcn_ballot_w64(open) == 0) return;
+    for (int e = 0; e < N; ++e) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = to_f32(x[u].v[e]);
+        const int key = k0 + u;
+        sum[e] += key >= first && key <= pos && key < k_end && !(fabsf(f) < INFINITY) ? f : 0.f;
+      }
+      open = open || ((all || y[e] != y[e]) && sum[e] == sum[e]);
+    }
+    if (__builtin_amdgcn_ballot_w64(open) == 0) break;
   }
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = (all || y[e] != y[e]) && sum[e] != 0.f ? sum[e] : y[e];
 }
 // Weight times a partial result, which stands whatever the weight where it is not finite
 __device__ __forceinline__ float weighed(float f, float y) { return fabsf(y) < INFINITY ? f * y : y; }

@@ -50,3 +50,17 @@ def test_values_that_are_not_finite_whatever_their_weight(dtype, hd, cached, fre
             want[i, 4:, 20] = NAN if sees(at) and sees(other) else top if sees(at) else -top
     assert torch.equal(torch.isnan(got), torch.isnan(want)), torch.isnan(got).ne(torch.isnan(want)).nonzero()[:4].tolist()
     assert torch.equal(got.nan_to_num(12345.0, INF, -INF), want.nan_to_num(12345.0, INF, -INF)), got.nan_to_num(12345.0, INF, -INF).ne(want.nan_to_num(12345.0, INF, -INF)).nonzero()[:4].tolist()
+
+
+@pytest.mark.parametrize("dtype,hd", [(F16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("cached,fresh,at", [(300, 1, 5), (9000, 1, 5), (300, 90, 5), (300, 90, 340), (9000, 40, 8000)])
+def test_a_key_whose_values_all_are_nan(dtype, hd, cached, fresh, at):
+    """Rows that see it are NaN in all dimensions of its head, the others keep their bits."""
+    s = R.Step([cached], [fresh], 16, 8, 2, hd, dtype, seed=6, stale=NAN)
+    s.make_plan()
+    s.K[int(s.full_table[0, at // 16]), 0, at % 16] = 0.0
+    before = s.attend().view(s.T, 8, hd)
+    s.V[int(s.full_table[0, at // 16]), 0, at % 16] = NAN
+    got = s.attend().view(s.T, 8, hd)
+    sees = torch.arange(cached, cached + fresh, device=got.device) >= at
+    assert torch.isnan(got[sees, :4]).all() and torch.equal(got[~sees], before[~sees]) and torch.equal(got[:, 4:], before[:, 4:])
