@@ -442,9 +442,13 @@ void attention_paged_16_kernel(const PagedAttn a) {
           float most = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) most = worst_of(v[e], most);
-          if ((signs >> 31 || most != most) && sum == sum)
+          if (__builtin_amdgcn_ballot_w64(((signs >> 31 != 0) | (most != most)) & (sum == sum)) != 0) {
+            float y[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
             settle<OT, HD>(a, table, Vh + d * 8, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
-                           window > 0 ? it.pos0 + t - window + 1 : 0, it.pos0 + t, signs >> 31, v);
+                           window > 0 ? it.pos0 + t - window + 1 : 0, it.pos0 + t, signs >> 31, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = y[e];
+          }
           if (it.part0 < 0) {
             const float inv = sum == 0.f ? 0.f : 1.0f / sum;
             vec8 y;
@@ -683,24 +687,37 @@ void attention_paged_16_kernel(const PagedAttn a) {
   for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) most = worst_of(o[t][e], most);
+  OT *const mine = (wave < 2 ? lV0 : lV1) + (wave & 1) * 32 * HD;          // LDS of the wave's own
   if (odd || __builtin_amdgcn_ballot_w64(most != most && l_tot == l_tot) != 0) {
+    // half of the sums at a time through LDS, a lane's own four side by side, so that a loop can take them: unrolled over the registers, this would
+    // be more code than the rest of the kernel
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(mine) + lane;
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t)
+    for (int t0 = 0; t0 < HD / 32; t0 += HD / 64) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float y[4] = {o[t][q * 4], o[t][q * 4 + 1], o[t][q * 4 + 2], o[t][q * 4 + 3]};
+      for (int i = 0; i < HD / 16; ++i)
+        sums[i * 64] = f32x4{o[t0 + i / 4][i % 4 * 4], o[t0 + i / 4][i % 4 * 4 + 1], o[t0 + i / 4][i % 4 * 4 + 2], o[t0 + i / 4][i % 4 * 4 + 3]};
+#pragma unroll 1
+      for (int i = 0; i < HD / 16; ++i) {
+        const f32x4 x = sums[i * 64];
+        float y[4] = {x[0], x[1], x[2], x[3]};
         if (!odd && __builtin_amdgcn_ballot_w64(y[0] != y[0] || y[1] != y[1] || y[2] != y[2] || y[3] != y[3]) == 0) continue;
-        settle<OT, HD>(a, table, Vh + t * 32 + q * 8 + half * 4, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
+        settle<OT, HD>(a, table, Vh + t0 * 32 + i * 8 + half * 4, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit,
                        window > 0 ? pos - window + 1 : 0, pos, odd, y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][q * 4 + e] = y[e];
+        sums[i * 64] = f32x4{y[0], y[1], y[2], y[3]};
       }
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        const f32x4 x = sums[i * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[t0 + i / 4][i % 4 * 4 + e] = x[e];
+      }
+    }
   }
   if (it.part0 < 0) {
     const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
-    // through LDS of the wave's own, so that a store is whole rows: stored from the accumulators, eight bytes of 32 rows at a time, 60
+    // through that LDS, so that a store is whole rows: stored from the accumulators, eight bytes of 32 rows at a time, 60
     // passages of 100 to 500 tokens take 165 us instead of 153
-    OT *const mine = (wave < 2 ? lV0 : lV1) + (wave & 1) * 32 * HD;
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t)
 #pragma unroll

@@ -250,7 +250,7 @@ void attention_paged_fp32_kernel(const PagedAttn a) {
       float most = 0.f;
 #pragma unroll
       for (int q = 0; q < 4; ++q) most = worst_of(y[q], most);
-      if ((signs >> 31 || most != most) && sum == sum) {
+      if (__builtin_amdgcn_ballot_w64(((signs >> 31 != 0) | (most != most)) & (sum == sum)) != 0) {
         float w[4] = {y[0], y[1], y[2], y[3]};
         settle<float, HD>(a, table, Vh + d, it.tile0 * 64, it.tile1 * 64 < limit ? it.tile1 * 64 : limit, window > 0 ? it.pos0 + t - window + 1 : 0,
                           it.pos0 + t, signs >> 31, w);
