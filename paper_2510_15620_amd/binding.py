@@ -455,7 +455,8 @@ class KVCache:
 
 class PagePlan:
     """The shape of a step (see prism_page_shape) and the device buffer of its plan.  Filled by op_page_plan, read by
-    op_attention_paged; may be filled again for another step of the same shape."""
+    op_attention_paged; may be filled again for another step of the same shape.  The buffer is made, and cleared, on the current
+    stream: as with any tensor, another stream waits for that one before it uses the plan."""
 
     def __init__(self, n_seqs: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, page_size: int, n_pages: int, max_pages: int,
                  window: int = 0):

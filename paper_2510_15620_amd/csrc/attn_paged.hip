@@ -8,12 +8,12 @@
 // per key; V^T's fragments come out of LDS by the transposing read (ds_read_b64_tr_b16), so that appending a token is a row's store.
 // P is rounded to the type of V, which the matrix cores ask for, and the denominators sum the rounded weights: 11 bits in half, as in
 // attn_16.hip, 8 in bf16, whose values half cannot hold.  Items of up to 32 rows, which wait for memory, take a bf16 weight as two numbers, the
-// second product with V costing nothing (100 sequences 315 us, 8.95 to 9.2 for three short ones); of more rows one, for there it would cost a fifth
+// second product with V costing nothing (100 sequences 315 us, 8.95 to 9.3 for three short ones); of more rows one, for there it would cost a fifth
 // (us: 32 heads of 128 with a cap 596 and 756, two chunks of 300 to 500 tokens 100 and 123, 60 passages 153 and 180).
 //
 // Two ways of dividing an item between its workgroup's four waves:
-//   more than 32 rows (chunks; bound by the power that matrix and vector work draw): 32 rows per wave, tiles of 64 keys shared through
-//     two LDS stages.  6900 tokens over up to 9700 each, 32 query heads over 8 of 128, half: 930 to 985 us, 860 to 915 TFLOP/s;
+//   more than 32 rows (chunks; matrix and vector work by turns, half of the cycles each): 32 rows per wave, tiles of 64 keys shared
+//     through two LDS stages.  6900 tokens over up to 9700 each, 32 query heads over 8 of 128, half: 910 to 990 us, 860 to 930 TFLOP/s;
 //   up to 32 rows (single tokens; HBM-bound): every wave takes all rows and its own 32 keys of every 128, through LDS of its own,
 //     without a barrier until the four partial results meet.  A token of 100 sequences over up to 8000 each: 1.76 GB in 315 us,
 //     5.6 TB/s; of one over 150 000: 0.61 GB in 115 us, 7 of them for joining.

@@ -4,7 +4,7 @@
 //
 // A workgroup of four waves takes 32 rows of an item.  Every wave has all of them, as two blocks of 16 that share a group of 16 keys in
 // registers, and every fourth group; the four meet in LDS.  What bounds it: the products keep the matrix pipes busy
-// for 17 us of the 56 that 40 ragged chunks over up to 900 keys take, 4 heads of 64; the rest is the softmax's instructions (some 120 to 32
+// for 17 us of the 54 that 40 ragged chunks over up to 900 keys take, 4 heads of 64; the rest is the softmax's instructions (some 120 to 32
 // products of 16 rows and keys) and compute units with a long chunk more than others.  With 16 rows per wave instead of 32 it was 76
 // to 70; head size 128, where two blocks spill, 164 to 285.  Weights are powers of 2 of scores in units of log 2: the factor's rounding
 // is 2^-25 of a score, as much as the score's own, and expf's range steps and exact splitting cost 9 us.
