@@ -31,6 +31,19 @@ def test_caps_of_every_size(dtype, nq, nkv, hd, cached, fresh, cap, scale):
     R.close(s.attend(scale, cap, slopes)[: s.cu[-1]], ref, _room(s, ref, scale, slopes))
 
 
+@pytest.mark.parametrize("dtype,nq,nkv,hd", [(F16, 8, 2, 128), (BF16, 14, 2, 64), (F32, 4, 2, 64)])
+@pytest.mark.parametrize("window", [0, 70])
+@pytest.mark.parametrize("cap,scale", [(100.0, 2.0), (1e5, 0.0), (1e20, 1.0)])
+def test_large_caps_with_slopes_windows_and_missing_pages(dtype, nq, nkv, hd, window, cap, scale):
+    s = R.Step([150, 20], [60, 1], 16, nq, nkv, hd, dtype, seed=14, window=window, stale=float("nan"))
+    s.make_plan()
+    s.full_table[0, 7] = -1
+    s.d_table = s.device(s.full_table)
+    slopes = torch.exp2(-8.0 * torch.arange(1, nq + 1) / nq).to(DEV)
+    ref, _ = R.attend(s.Q, s.K, s.V, s.full_table, s.cached, s.cu, nq, nkv, hd, scale, cap, window, slopes, dtype)
+    R.close(s.attend(scale, cap, slopes)[: s.cu[-1]], ref, _room(s, ref, scale, slopes))
+
+
 @pytest.mark.parametrize("dtype,hd", [(F16, 128), (F16, 64), (BF16, 128), (F32, 64)])
 @pytest.mark.parametrize("fresh", [1, 40])
 @pytest.mark.parametrize("cap,factor", [(1e4, 1e3), (1e5, 1e4), (1e5, 2e3)])

@@ -53,14 +53,15 @@ def test_values_that_are_not_finite_whatever_their_weight(dtype, hd, cached, fre
 
 
 @pytest.mark.parametrize("dtype,hd", [(F16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("softcap", [0.0, 30.0, 1000.0])
 @pytest.mark.parametrize("cached,fresh,at", [(300, 1, 5), (9000, 1, 5), (300, 90, 5), (300, 90, 340), (9000, 40, 8000)])
-def test_a_key_whose_values_all_are_nan(dtype, hd, cached, fresh, at):
+def test_a_key_whose_values_all_are_nan(dtype, hd, cached, fresh, at, softcap):
     """Rows that see it are NaN in all dimensions of its head, the others keep their bits."""
     s = R.Step([cached], [fresh], 16, 8, 2, hd, dtype, seed=6, stale=NAN)
     s.make_plan()
     s.K[int(s.full_table[0, at // 16]), 0, at % 16] = 0.0
-    before = s.attend().view(s.T, 8, hd)
+    before = s.attend(softcap=softcap).view(s.T, 8, hd)
     s.V[int(s.full_table[0, at // 16]), 0, at % 16] = NAN
-    got = s.attend().view(s.T, 8, hd)
+    got = s.attend(softcap=softcap).view(s.T, 8, hd)
     sees = torch.arange(cached, cached + fresh, device=got.device) >= at
     assert torch.isnan(got[sees, :4]).all() and torch.equal(got[~sees], before[~sees]) and torch.equal(got[:, 4:], before[:, 4:])
