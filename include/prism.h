@@ -381,6 +381,40 @@ int prism_op_attention_paged(const prism_page_shape *shape, const prism_kv_cache
                              const void *Q, int64_t q_stride, float scale, float softcap, const float *slopes, void *out,
                              int64_t out_stride, void *workspace, int64_t workspace_bytes, void *stream);
 
+/* ---- 8-bit rows ------------------------------------------------------------------------------------------------------
+ * Products whose operands are 8-bit integers with a scale a row: half the bytes of 16-bit weights, twice the rate of the matrix cores.  A layer's block is
+ * prism_op_rmsnorm_q8, then prism_op_gemm_q8; prism_op_quantize_q8 makes rows of what comes in 16 bits or fp32 (attention output, SwiGLU
+ * output; weights, once, a row being an output channel).  None of them allocates or synchronises: all can be captured into a graph.
+ *
+ * Row r stands for the numbers codes[r * stride + c] * scales[r], c < cols, with scale = max|x| / 127 and code = x / scale rounded to the nearest integer,
+ * ties to even.  A row with a NaN or an infinity has a scale of NaN and codes of 0, so that what is computed of it is NaN; a row whose largest magnitude is below
+ * 2^-119 has a scale of 0 and codes of 0.  Codes behind cols are 0 up to a multiple of 128 (the makers write them; a caller's own rows have to
+ * have them, and may have codes of -128). */
+typedef struct {
+  int8_t *codes;                      /* [device], 16-byte aligned */
+  float  *scales;                     /* [device] [rows] */
+  int64_t stride;                     /* bytes from row to row: a multiple of 16, at least cols rounded up to 128, at most 2^23 */
+  int32_t rows, cols;                 /* rows 0..PRISM_MAX_STEP; cols 1..131071 (a product's sums fit 32 bits) */
+} prism_q8;
+
+/* Rows of out->cols numbers of dtype (FP32, BF16, F16), x_stride values apart (up to 2^23), to codes and scales.  Codes of 16-bit rows are exact; of fp32 rows, x / scale
+ * is off by 2^-23 of itself at most before it is rounded. */
+int prism_op_quantize_q8(int32_t dtype, const void *X, int64_t x_stride, const prism_q8 *out, void *stream);
+/* code * scale in fp32, rounded once more to 16 bits (half saturates, NaN stays NaN), to rows out_stride values apart. */
+int prism_op_dequantize_q8(const prism_q8 *q, int32_t dtype, void *out, int64_t out_stride, void *stream);
+
+/* Residual addition, RMSNorm and quantisation in one pass: X[t,:] += add[t,:] (fp32, stored; add may be NULL), then the rows of X / sqrt(mean(X^2) + eps) * gain to
+ * out (out->rows rows of out->cols).  add and gain [cols] of any dtype each.  The normed values are not rounded before they are quantised.  1e-30 <= eps < 1e30.
+ * A row whose squares' sum is beyond fp32 counts as one with an infinity.  add must not overlap X. */
+int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype, const void *add, int64_t add_stride, int32_t gain_dtype, const void *gain,
+                        float eps, const prism_q8 *out, void *stream);
+
+/* Y[m,n] = A.scales[m] W.scales[n] sum_k A[m,k] W[n,k] with the epilogues of prism_op_gemm: STORE and SWIGLU to BF16 or F16 (half saturates, NaN stays NaN),
+ * STORE_F32 and RESIDUAL to FP32; out has A->rows rows of W->rows values (SWIGLU: half as many), out_stride values apart (up to 2^23).  The sum of
+ * integers is exact, everything behind it is fp32.  W's rows together are below 4 GiB - 8 KiB.  out must not overlap the operands.
+ * The order of nothing depends on timing: same inputs, same bits. */
+int prism_op_gemm_q8(int32_t epilogue, const prism_q8 *A, const prism_q8 *W, int32_t out_dtype, void *out, int64_t out_stride, void *stream);
+
 /* Intermediate scorer (Sec. 4.1): for each sequence c, the last token's state through the final RMSNorm and
  * the yes/no head: scores[c] = z . w_yes - z . w_no.  last_row[c] = row of that token in X (NULL: row c). */
 int prism_op_score(const float *X, const int32_t *last_row, int32_t n_seqs, int32_t hidden,

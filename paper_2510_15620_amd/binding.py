@@ -26,7 +26,8 @@ EXPORTS = ["prism_create", "prism_select", "prism_set_forced_keep", "prism_destr
            "prism_last_error", "prism_op_embed", "prism_op_rmsnorm", "prism_op_gemm", "prism_op_qkv_finish", "prism_op_qkv_project", "prism_w4_bytes", "prism_op_quantize_w4", "prism_op_dequantize_w4",
            "prism_op_attention", "prism_op_score", "prism_op_route", "prism_op_route_static", "prism_op_compact", "prism_op_topk", "prism_vt_column_of_key",
            "prism_page_plan_bytes", "prism_op_page_plan", "prism_op_qkv_finish_paged", "prism_attention_paged_workspace",
-           "prism_op_attention_paged"]
+           "prism_op_attention_paged",
+           "prism_op_quantize_q8", "prism_op_dequantize_q8", "prism_op_rmsnorm_q8", "prism_op_gemm_q8"]
 
 
 class PrismError(RuntimeError):
@@ -66,6 +67,10 @@ class prism_kv_cache(C.Structure):
 
 class prism_page_shape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_seqs", "n_tokens", "n_q_heads", "n_kv_heads", "page_size", "n_pages", "max_pages", "window")]
+
+
+class prism_q8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("stride", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
 
 
 class prism_report(C.Structure):
@@ -132,6 +137,11 @@ def lib() -> C.CDLL:
         _lib.prism_attention_paged_workspace.restype = i64
         _lib.prism_attention_paged_workspace.argtypes = [shape, i32]
         _lib.prism_op_attention_paged.argtypes = [shape, cache, vp, vp, vp, i64, f32, f32, vp, vp, i64, vp, i64, vp]
+        q8 = C.POINTER(prism_q8)
+        _lib.prism_op_quantize_q8.argtypes = [i32, vp, i64, q8, vp]
+        _lib.prism_op_dequantize_q8.argtypes = [q8, i32, vp, i64, vp]
+        _lib.prism_op_rmsnorm_q8.argtypes = [vp, i64, i32, vp, i64, i32, vp, f32, q8, vp]
+        _lib.prism_op_gemm_q8.argtypes = [i32, q8, q8, i32, vp, i64, vp]
     return _lib
 
 
@@ -423,7 +433,7 @@ def _gain(t, hd: int, dtype, device: int) -> int:
     raise PrismError(EINVAL, f"a gain of {hd} values of {dtype} on the current device")
 
 
-_torch = None               # set with the first cache or plan: the calls below have both at hand and are short
+_torch = None               # set with the first cache, plan or 8-bit rows: the calls below have one at hand and are short
 
 
 def _here():
@@ -526,3 +536,103 @@ def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace,
     _check(lib().prism_op_attention_paged(
         plan._ref, cache._ref, plan.buffer.data_ptr(), _table(table, plan, d), q, q_stride, scale, softcap,
         0 if slopes is None else slopes.data_ptr(), o, o_stride, workspace.data_ptr(), workspace.nbytes, stream))
+
+
+# ---- 8-bit rows ---------------------------------------------------------------------------------------------------------
+
+_DTYPES = {}                # torch dtype -> PRISM_DTYPE_*, filled with the first rows
+
+
+class Q8:
+    """Rows of 8-bit codes with a scale each (see prism_q8), on the current device: made by op_rmsnorm_q8 and op_quantize_q8, read by
+    op_gemm_q8 and op_dequantize_q8.  codes [rows, stride] int8, stride being cols rounded up to 128; scales [rows] fp32.  Uninitialised.
+    Keep weights in one for as long as they are used, and activations in one for each place that may be in use at the same time."""
+
+    def __init__(self, rows: int, cols: int):
+        import torch
+        _need(rows >= 0 and cols > 0, f"Q8: {rows} rows of {cols} codes")
+        self._set(torch.empty(rows, (cols + 127) // 128 * 128, dtype=torch.int8, device="cuda"),
+                  torch.empty(rows, dtype=torch.float32, device="cuda"), cols)
+
+    def _set(self, codes, scales, cols):
+        global _torch
+        import torch
+        _torch = torch
+        if not _DTYPES:
+            _DTYPES.update({torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16})
+        self.codes, self.scales, self.cols, self.rows, self.device = codes, scales, cols, codes.shape[0], codes.get_device()
+        self._c = prism_q8(codes.data_ptr(), scales.data_ptr(), codes.shape[1], self.rows, cols)
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def of(cls, codes, scales) -> "Q8":
+        """A copy of codes [rows, cols] int8 and scales [rows] fp32 (weights quantised elsewhere, say) in this layout."""
+        import torch
+        _need(codes.dim() == 2 and codes.dtype is torch.int8 and codes.is_cuda and codes.get_device() == torch.cuda.current_device(),
+              "Q8.of: codes [rows, cols] int8 on the current device")
+        _need(scales.shape == codes.shape[:1] and scales.dtype is torch.float32 and scales.device == codes.device, "Q8.of: a fp32 scale for each row")
+        q = cls(*codes.shape)
+        q.codes[:, codes.shape[1]:] = 0
+        q.codes[:, :codes.shape[1]] = codes
+        q.scales.copy_(scales)
+        return q
+
+    def first(self, rows: int) -> "Q8":
+        """The first `rows` rows, in place: a buffer made for the largest batch serves smaller ones."""
+        _need(0 <= rows <= self.rows, f"Q8.first: {rows} of {self.rows} rows")
+        q = Q8.__new__(Q8)
+        q._set(self.codes[:rows], self.scales[:rows], self.cols)
+        return q
+
+
+def _any_rows(t, rows: int, cols: int, device: int, what: str):
+    """Address, row stride and dtype number of a device tensor [rows, cols] whose rows are dense."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is not None and t.dim() == 2 and t.get_device() == device:
+        n, width = t.shape
+        stride, one = t.stride()
+        if n == rows and width == cols and (one == 1 or width < 2):
+            return t.data_ptr(), stride if n > 1 else width, dtype
+    raise PrismError(EINVAL, f"{what}: [{rows}, {cols}] in fp32, bf16 or half, rows dense, on the current device")
+
+
+def op_quantize_q8(X, out: Q8):
+    """X [rows, cols] fp32, bf16 or half -> out."""
+    d, stream = _here()
+    x, x_stride, dtype = _any_rows(X, out.rows, out.cols, d, "op_quantize_q8: X")
+    _check_q8_device(out, d)
+    _check(lib().prism_op_quantize_q8(dtype, x, x_stride, out._ref, stream))
+
+
+def op_dequantize_q8(q: Q8, out):
+    """q -> out [rows, cols] fp32, bf16 or half."""
+    d, stream = _here()
+    o, o_stride, dtype = _any_rows(out, q.rows, q.cols, d, "op_dequantize_q8: out")
+    _check_q8_device(q, d)
+    _check(lib().prism_op_dequantize_q8(q._ref, dtype, o, o_stride, stream))
+
+
+def op_rmsnorm_q8(X, gain, eps, out: Q8, add=None):
+    """X [rows, cols] fp32 (+= add, any dtype, where given), normed and quantised to out; gain [cols], any dtype."""
+    d, stream = _here()
+    x, x_stride, dtype = _any_rows(X, out.rows, out.cols, d, "op_rmsnorm_q8: X")
+    gain_dtype = _DTYPES.get(gain.dtype)
+    if dtype != DTYPE_FP32 or gain_dtype is None or gain.numel() != out.cols or not gain.is_contiguous() or gain.get_device() != d:
+        raise PrismError(EINVAL, f"op_rmsnorm_q8: X in fp32 and a gain of {out.cols} values on the current device")
+    a, a_stride, add_dtype = (0, 0, 0) if add is None else _any_rows(add, out.rows, out.cols, d, "op_rmsnorm_q8: add")
+    _check_q8_device(out, d)
+    _check(lib().prism_op_rmsnorm_q8(x, x_stride, add_dtype, a, a_stride, gain_dtype, gain.data_ptr(), eps, out._ref, stream))
+
+
+def op_gemm_q8(epilogue, A: Q8, W: Q8, out):
+    """out [A.rows, W.rows] (EPI_SWIGLU: W.rows / 2 columns) = epilogue of A W^T: bf16 or half for EPI_STORE and EPI_SWIGLU, else fp32."""
+    d, stream = _here()
+    _check_q8_device(A, d)
+    _check_q8_device(W, d)
+    o, o_stride, dtype = _any_rows(out, A.rows, W.rows // 2 if epilogue == EPI_SWIGLU else W.rows, d, "op_gemm_q8: out")
+    _check(lib().prism_op_gemm_q8(epilogue, A._ref, W._ref, dtype, o, o_stride, stream))
+
+
+def _check_q8_device(q: Q8, device: int):
+    if q.device != device:
+        raise PrismError(EINVAL, "8-bit rows on another device than the current one")

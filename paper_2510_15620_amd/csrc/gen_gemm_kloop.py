@@ -3,6 +3,9 @@
 
     python gen_gemm_kloop.py > gemm_16_kloop.inc        (the output is committed too)
 
+A loop sees bytes: slices of 128 bytes a row, fragments of 16 bytes a lane.  The matrix instruction is its parameter: 16x16x32 on 16-bit
+values or 16x16x64 on 8-bit integers, which take the same registers and cycles; below, k counts 16-bit values.
+
 The 256x256x64 tile.  4 wavefronts (one per SIMD, so each owns 512 registers), wave grid 2x2, wave tile 128x128 = 8x8
 accumulator tiles of v_mfma_f32_16x16x32 kept in 256 AGPRs: the largest wave tile the register file allows, i.e. the
 fewest LDS bytes per MFMA.  A slice is 64 deep: 2 steps of 64 MFMAs (16 cycles each, 2048 in all).
@@ -65,7 +68,7 @@ def reads(fs, k, t):
 
 
 def mfma(fs, i, j):
-    return f'v_mfma_f32_16x16x32_" TY " {acc(i, j)}, {v4(F[fs]["B"][j])}, {v4(F[fs]["A"][i])}, {acc(i, j)}'
+    return f'v_mfma_" TY " {acc(i, j)}, {v4(F[fs]["B"][j])}, {v4(F[fs]["A"][i])}, {acc(i, j)}'
 
 
 def load_group(which, n, lds_off, m0_at=0):
@@ -260,7 +263,7 @@ class Small:
                     s += [f"s_waitcnt {outstanding}"]
                 (i, j), u = order[m % NS], 2 * t + m // NS
                 r = (i * self.TN + j) * 4
-                s.append(f'v_mfma_f32_16x16x32_" TY " a[{r}:{r + 3}], {self.frag(u, "B", j)}, {self.frag(u, "A", i)}, a[{r}:{r + 3}]')
+                s.append(f'v_mfma_" TY " a[{r}:{r + 3}], {self.frag(u, "B", j)}, {self.frag(u, "A", i)}, a[{r}:{r + 3}]')
                 s += behind.get(m, [])
             s += ["s_sub_u32 s24, s24, 1"] + (["s_cbranch_scc1 L_done_%="] if t + 1 < period else ["s_cbranch_scc0 L_loop_%="])
         s += ["L_done_%=:", "s_waitcnt vmcnt(0) lgkmcnt(0)", "s_nop 15", "s_nop 15"]
@@ -304,7 +307,7 @@ def emit(name, lines):
 
 def main():
     print("// Generated by gen_gemm_kloop.py - do not edit.  See that file for the schedule.")
-    print("// PRISM_KLOOP_<tile>(TY), TY = \"f16\" or \"bf16\": accumulators a[0:...], tile (i, j) of 16 x 16 in the four from 4 (TN i + j) on;")
+    print("// PRISM_KLOOP_<tile>(TY), TY = \"f32_16x16x32_f16\", \"f32_16x16x32_bf16\" or \"i32_16x16x64_i8\": accumulators a[0:...], tile (i, j) of 16 x 16 in the four from 4 (TN i + j) on;")
     print("// aa / ab / ab2 LDS byte address of the lane's first fragment row of A, of the lower and of the upper half of the wave's B columns")
     print("// (step 0, stage 0); ga / gb byte offset from pa / pb of the chunk this lane fetches in each of its wave's load instructions,")
     print("// less 1024 (j % 4); la / lb LDS byte address of the first row the first of them fills (stage 0, uniform); nk number of slices.")
