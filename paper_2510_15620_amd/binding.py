@@ -433,7 +433,7 @@ def _gain(t, hd: int, dtype, device: int) -> int:
     raise PrismError(EINVAL, f"a gain of {hd} values of {dtype} on the current device")
 
 
-_torch = None               # set with the first cache, plan or 8-bit rows: the calls below have one at hand and are short
+_torch = None               # set with the first cache or plan: the calls below have both at hand and are short
 
 
 def _here():
@@ -540,7 +540,9 @@ def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace,
 
 # ---- 8-bit rows ---------------------------------------------------------------------------------------------------------
 
-_DTYPES = {}                # torch dtype -> PRISM_DTYPE_*, filled with the first rows
+# Set with the first rows, by which every call gets here: a step of a few tokens waits for the host, so that these calls look nothing up twice
+_DTYPES = {}                # torch dtype -> PRISM_DTYPE_*
+_device = _raw_stream = None
 
 
 class Q8:
@@ -555,12 +557,14 @@ class Q8:
                   torch.empty(rows, dtype=torch.float32, device="cuda"), cols)
 
     def _set(self, codes, scales, cols):
-        global _torch
-        import torch
-        _torch = torch
+        global _device, _raw_stream
         if not _DTYPES:
+            import torch
+            lib()
+            _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
             _DTYPES.update({torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16})
-        self.codes, self.scales, self.cols, self.rows, self.device = codes, scales, cols, codes.shape[0], codes.get_device()
+        self.codes, self.scales, self.rows, self.cols, self.shape = codes, scales, codes.shape[0], cols, (codes.shape[0], cols)
+        self.device = codes.get_device()
         self._c = prism_q8(codes.data_ptr(), scales.data_ptr(), codes.shape[1], self.rows, cols)
         self._ref = C.byref(self._c)
 
@@ -585,54 +589,63 @@ class Q8:
         return q
 
 
-def _any_rows(t, rows: int, cols: int, device: int, what: str):
-    """Address, row stride and dtype number of a device tensor [rows, cols] whose rows are dense."""
+def _any_rows(t, shape, device: int, what: str):
+    """Address, row stride and dtype number of a device tensor of that shape whose rows are dense."""
     dtype = _DTYPES.get(t.dtype)
-    if dtype is not None and t.dim() == 2 and t.get_device() == device:
-        n, width = t.shape
+    if dtype is not None and t.shape == shape and t.get_device() == device:
         stride, one = t.stride()
-        if n == rows and width == cols and (one == 1 or width < 2):
-            return t.data_ptr(), stride if n > 1 else width, dtype
-    raise PrismError(EINVAL, f"{what}: [{rows}, {cols}] in fp32, bf16 or half, rows dense, on the current device")
+        if one == 1 or shape[1] < 2:
+            return t.data_ptr(), stride if shape[0] > 1 else shape[1], dtype
+    raise PrismError(EINVAL, f"{what}: {list(shape)} in fp32, bf16 or half, rows dense, on the current device")
+
+
+def _elsewhere():
+    raise PrismError(EINVAL, "8-bit rows on another device than the current one")
 
 
 def op_quantize_q8(X, out: Q8):
     """X [rows, cols] fp32, bf16 or half -> out."""
-    d, stream = _here()
-    x, x_stride, dtype = _any_rows(X, out.rows, out.cols, d, "op_quantize_q8: X")
-    _check_q8_device(out, d)
-    _check(lib().prism_op_quantize_q8(dtype, x, x_stride, out._ref, stream))
+    d = _device()
+    x, x_stride, dtype = _any_rows(X, out.shape, d, "op_quantize_q8: X")
+    if out.device != d:
+        _elsewhere()
+    rc = _lib.prism_op_quantize_q8(dtype, x, x_stride, out._ref, _raw_stream(d))
+    if rc:
+        _check(rc)
 
 
 def op_dequantize_q8(q: Q8, out):
     """q -> out [rows, cols] fp32, bf16 or half."""
-    d, stream = _here()
-    o, o_stride, dtype = _any_rows(out, q.rows, q.cols, d, "op_dequantize_q8: out")
-    _check_q8_device(q, d)
-    _check(lib().prism_op_dequantize_q8(q._ref, dtype, o, o_stride, stream))
+    d = _device()
+    o, o_stride, dtype = _any_rows(out, q.shape, d, "op_dequantize_q8: out")
+    if q.device != d:
+        _elsewhere()
+    rc = _lib.prism_op_dequantize_q8(q._ref, dtype, o, o_stride, _raw_stream(d))
+    if rc:
+        _check(rc)
 
 
 def op_rmsnorm_q8(X, gain, eps, out: Q8, add=None):
     """X [rows, cols] fp32 (+= add, any dtype, where given), normed and quantised to out; gain [cols], any dtype."""
-    d, stream = _here()
-    x, x_stride, dtype = _any_rows(X, out.rows, out.cols, d, "op_rmsnorm_q8: X")
+    d = _device()
+    x, x_stride, dtype = _any_rows(X, out.shape, d, "op_rmsnorm_q8: X")
     gain_dtype = _DTYPES.get(gain.dtype)
-    if dtype != DTYPE_FP32 or gain_dtype is None or gain.numel() != out.cols or not gain.is_contiguous() or gain.get_device() != d:
+    if dtype or gain_dtype is None or gain.numel() != out.cols or not gain.is_contiguous() or gain.get_device() != d:
         raise PrismError(EINVAL, f"op_rmsnorm_q8: X in fp32 and a gain of {out.cols} values on the current device")
-    a, a_stride, add_dtype = (0, 0, 0) if add is None else _any_rows(add, out.rows, out.cols, d, "op_rmsnorm_q8: add")
-    _check_q8_device(out, d)
-    _check(lib().prism_op_rmsnorm_q8(x, x_stride, add_dtype, a, a_stride, gain_dtype, gain.data_ptr(), eps, out._ref, stream))
+    a, a_stride, add_dtype = (0, 0, 0) if add is None else _any_rows(add, out.shape, d, "op_rmsnorm_q8: add")
+    if out.device != d:
+        _elsewhere()
+    rc = _lib.prism_op_rmsnorm_q8(x, x_stride, add_dtype, a, a_stride, gain_dtype, gain.data_ptr(), eps, out._ref, _raw_stream(d))
+    if rc:
+        _check(rc)
 
 
 def op_gemm_q8(epilogue, A: Q8, W: Q8, out):
     """out [A.rows, W.rows] (EPI_SWIGLU: W.rows / 2 columns) = epilogue of A W^T: bf16 or half for EPI_STORE and EPI_SWIGLU, else fp32."""
-    d, stream = _here()
-    _check_q8_device(A, d)
-    _check_q8_device(W, d)
-    o, o_stride, dtype = _any_rows(out, A.rows, W.rows // 2 if epilogue == EPI_SWIGLU else W.rows, d, "op_gemm_q8: out")
-    _check(lib().prism_op_gemm_q8(epilogue, A._ref, W._ref, dtype, o, o_stride, stream))
-
-
-def _check_q8_device(q: Q8, device: int):
-    if q.device != device:
-        raise PrismError(EINVAL, "8-bit rows on another device than the current one")
+    d = _device()
+    o, o_stride, dtype = _any_rows(out, (A.rows, W.rows // 2 if epilogue == EPI_SWIGLU else W.rows), d, "op_gemm_q8: out")
+    if A.device != d or W.device != d:
+        _elsewhere()
+    rc = _lib.prism_op_gemm_q8(epilogue, A._ref, W._ref, dtype, o, o_stride, _raw_stream(d))
+    if rc:
+        _check(rc)

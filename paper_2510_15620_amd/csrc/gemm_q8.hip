@@ -8,7 +8,6 @@
 #include <algorithm>
 
 #include "gemm_tile.h"
-#include "q8.h"
 
 namespace prism {
 
@@ -103,6 +102,7 @@ extern "C" int prism_op_gemm_q8(int32_t epilogue, const prism_q8 *A, const prism
   if (A->rows == 0 || cols == 0) return PRISM_OK;
   PRISM_REQUIRE(out && (uintptr_t)out % (wide ? 4 : 2) == 0, PRISM_EINVAL, "gemm_q8: output missing or not aligned to its values");
   hipStream_t s = (hipStream_t)stream;
+  if (gemm_q8_few_rows(A->rows, W->rows, A->cols)) return launch_gemm_q8_rows(epilogue, *A, *W, out_dtype, out, out_stride, s);
   const bool half = out_dtype == PRISM_DTYPE_F16;
   switch (epilogue) {
     case PRISM_EPI_STORE: return half ? launch_epi<f16, PRISM_EPI_STORE>(*A, *W, out, out_stride, s) : launch_epi<bf16, PRISM_EPI_STORE>(*A, *W, out, out_stride, s);

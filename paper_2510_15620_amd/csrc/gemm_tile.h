@@ -26,6 +26,7 @@
 
 #include "common.h"
 #include "gemm_16_kloop.inc"
+#include "gemm_q8.h"
 
 namespace prism {
 
@@ -40,22 +41,8 @@ __device__ __forceinline__ int swz(int row, int chunk) { return chunk ^ ((row >>
 #define PRISM_GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
 #define PRISM_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 
-// silu(g) * u in fp32, rounded to 16 bits by its callers.  The division is correctly rounded: a product with the reciprocal
-// instruction takes half of this epilogue's arithmetic away (13.8 -> 9.2 thousand cycles of a 256 x 256 tile) and no time where the
-// chip is full and at its power limit (24576 x 24576 x 4096: 3350 us, with the division 3337), but is off by
-// an ulp more and returns 0 where 1 + e^-g exceeds 2^126, values that bf16 still holds.
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
-
 // LDS bytes of a tile's operand stages
 template <int BM, int BN, int S> constexpr int stage_bytes() { return ((BM == 256 ? 3 : S) * BM + S * BN) * BK * 2; }
-
-// What a product of 8-bit rows brings: a scale for each row of A and of W, the distance of the rows in bytes (multiples of 16), and
-// the distance of the output's rows in values.
-struct Q8Operands {
-  const float *sa, *sw;
-  uint32_t lda, ldw;
-  int64_t ldo;
-};
 
 // OT: type of 16-bit operands and outputs; IT: the operands' (OT or int8_t)
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT = OT>
@@ -246,11 +233,9 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
       return r;
     }
   };
-  // to 16 bits; 8-bit products keep a NaN (of a row without a scale), which half's saturation would turn into a number
   auto to16 = [&](float v) __attribute__((always_inline)) {
-    const OT r = from_f32<OT>(v);
-    if constexpr (kQ8 && std::is_same_v<OT, f16>) return v == v ? r : (OT)v;
-    else return r;
+    if constexpr (kQ8) return q8_round<OT>(v);
+    else return from_f32<OT>(v);
   };
   __syncthreads();              // every wave's operand loads have landed and nobody reads operands any more
   constexpr int SWZ = CPR >= 16 ? 15 : CPR - 1;                     // chunk rotation by row: spreads a column of 16-byte

@@ -4,7 +4,7 @@
 // A row x has scale = max|x| / 127 and codes x / scale, rounded to the nearest integer, ties to even.  The norm's rows are n = x r gain with one r a row, which
 // cancels in n / scale: code = x gain 127 / max|x gain|, so the sum of squares (for r) and the maximum meet in one reduction and the row is read once.
 // All of it is bound by memory; rows stay in registers between the maximum and the codes.
-#include "q8.h"
+#include "gemm_q8.h"
 
 namespace prism {
 
@@ -198,8 +198,6 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_q8_kernel(NormArgs a) {
 }
 
 // ---- back to numbers: code * scale, rounded once more to 16 bits.  256 threads take 8 codes each, of 256 / lanes rows
-template <typename T> __device__ __forceinline__ T round_value(float v) { return from_f32<T>(v); }
-template <> __device__ __forceinline__ f16 round_value<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }   // half saturates, NaN stays
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_q8_kernel(const int8_t *__restrict__ codes, int64_t stride, const float *__restrict__ scales, int rows, int cols, int lanes,
                                                             T *__restrict__ out, int64_t out_stride) {
@@ -212,7 +210,7 @@ __global__ __launch_bounds__(256) void dequantize_q8_kernel(const int8_t *__rest
     const uint2 c = *reinterpret_cast<const uint2 *>(in + i);
     typename Pack<T, 8>::vec v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = round_value<T>((float)(int8_t)((e < 4 ? c.x : c.y) >> (e & 3) * 8) * s);
+    for (int e = 0; e < 8; ++e) v[e] = q8_round<T>((float)(int8_t)((e < 4 ? c.x : c.y) >> (e & 3) * 8) * s);
     if (i + 8 <= cols) *reinterpret_cast<typename Pack<T, 8>::any *>(o + i) = v;
     else
       for (int e = 0; e < 8; ++e)
