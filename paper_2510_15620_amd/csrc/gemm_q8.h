@@ -6,11 +6,12 @@
 namespace prism {
 
 // What a product of 8-bit rows brings: a scale for each row of A and of W, the distance of the rows in bytes (multiples of 16), and
-// the distance of the output's rows in values.
+// the distance of the output's rows in values; of the tiles, by how many slices of K a column tile begins behind the one before it (0: all begin at K's start).
 struct Q8Operands {
   const float *sa, *sw;
   uint32_t lda, ldw;
   int64_t ldo;
+  int turn;
 };
 
 // silu(g) * u in fp32, rounded to 16 bits by its callers.  The division is correctly rounded: a product with the reciprocal
@@ -23,8 +24,7 @@ __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f +
 template <typename T> __device__ __forceinline__ T q8_round(float v) { return from_f32<T>(v); }
 template <> __device__ __forceinline__ f16 q8_round<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }
 
-// Products of few rows (gemm_q8_rows.hip): whether one of M rows of A and N of W goes there, and its launch (M <= 64, arguments checked)
-bool gemm_q8_few_rows(int M, int N, int K);
+// Products of few rows, up to 64 (gemm_q8_rows.hip; arguments checked)
 int launch_gemm_q8_rows(int epilogue, const prism_q8 &a, const prism_q8 &w, int out_dtype, void *out, int64_t out_stride, hipStream_t s);
 
 }  // namespace prism

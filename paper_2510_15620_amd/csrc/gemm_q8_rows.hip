@@ -141,23 +141,13 @@ template <typename OT, int EPI, int MT, int NT, int NW, int D>
 static int launch(const prism_q8 &a, const prism_q8 &w, void *out, int64_t out_stride, hipStream_t s) {
   constexpr int NO = EPI == PRISM_EPI_SWIGLU ? NT / 2 : NT;
   const int F = EPI == PRISM_EPI_SWIGLU ? w.rows / 2 : w.rows, width = q8_width(a.cols);
-  const Q8Operands q{a.scales, w.scales, (uint32_t)a.stride, (uint32_t)w.stride, out_stride};
+  const Q8Operands q{a.scales, w.scales, (uint32_t)a.stride, (uint32_t)w.stride, out_stride, 0};
   gemm_q8_rows_kernel<OT, EPI, MT, NT, NW, D><<<cdiv(F, NO * 16), NW * 64, 0, s>>>(a.codes, w.codes, out, a.rows, w.rows, width / kQ8Slice,
                                                                                   (uint32_t)((a.rows - 1) * a.stride + width), (uint32_t)((w.rows - 1) * w.stride + width), q);
   PRISM_HIP(hipGetLastError());
   return PRISM_OK;
 }
 
-// Which launches run here; the others take tiles.  A load of the matrix instruction's rows touches 16 cache lines with 64 bytes in each, where the tiles' loads
-// into LDS take 8 whole lines, and a compute unit looks up a line in some 4 cycles: nothing for weights, which memory brings at 8 bytes a cycle
-// and unit, but every 16 rows of A cost as much again.  us, weights from memory, here / on tiles: 1 x 4096 x 4096 5.5 / 7.0, 16 x 4096 x 4096 6.5 / 7.5,
-// 1 x 12288 x 8192 22.9 / 25.1, 16 x 12288 x 8192 28.8 / 24.1, 16 x 512 x 8192 9.0 / 8.2, 1 x 512 x 512 2.0 / 3.1; 32 x 4096 x 1024 3.7 / 4.7, 32 x 12288 x 1024 7.2 / 6.3, 32 x
-// 4096 x 4096 8.6 / 8.4; 64 x 2048 x 512 3.5 / 3.9, 64 x 4096 x 1024 4.6 / 4.8, 64 x 512 x 2048 6.3 / 4.2; SwiGLU 24 x 6144 x 1024 4.8 / 5.9, 1 x 24576 x 4096 20.5 / 26.1.
-bool gemm_q8_few_rows(int M, int N, int K) {
-  if (M <= 8) return true;
-  if (M <= 16) return (int64_t)N * K < 48000000 && (K <= 2048 || N >= 2048);
-  return M <= 64 && K <= 1024 && N <= (M <= 32 ? 8192 : 4096);
-}
 // One column tile a wave (SwiGLU two): more of them in fewer workgroups were slower, 16 x 4096 x 4096 8.6 for two, 14.7 for four.  Slices of K: up to 8, 4 waves; from 32 on, four ahead (1 x
 // 24576 x 4096 with SwiGLU 22.3 -> 20.5; on 8 and fewer slices that would ask for slices that are not there, 1 x 1024 x 1024 3.1 -> 3.6).
 template <typename OT, int EPI>

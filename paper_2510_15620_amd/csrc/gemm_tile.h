@@ -26,6 +26,7 @@
 
 #include "common.h"
 #include "gemm_16_kloop.inc"
+#include "gemm_q8_kloop.inc"
 #include "gemm_q8.h"
 
 namespace prism {
@@ -42,7 +43,7 @@ __device__ __forceinline__ int swz(int row, int chunk) { return chunk ^ ((row >>
 #define PRISM_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 
 // LDS bytes of a tile's operand stages
-template <int BM, int BN, int S> constexpr int stage_bytes() { return ((BM == 256 ? 3 : S) * BM + S * BN) * BK * 2; }
+template <int BM, int BN, int S> constexpr int stage_bytes() { return ((BN == 256 ? 3 : S) * BM + S * BN) * BK * 2; }
 
 // OT: type of 16-bit operands and outputs; IT: the operands' (OT or int8_t)
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT = OT>
@@ -61,9 +62,10 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   static_assert(EPI != PRISM_EPI_SWIGLU || TN % 2 == 0, "SwiGLU pairs gate and up tiles");
   static_assert(TM * TN * 4 <= 256, "accumulator registers");
   extern __shared__ __align__(16) unsigned char smem[];
-  static_assert(BM != 256 || S == 2, "the 256 x 256 loop has three stages of A and two of W");
-  unsigned char *lA = smem;                                          // [S, or 3 if BM == 256][BM][BK] of two bytes
-  unsigned char *lB = lA + (BM == 256 ? 3 : S) * BM * BK * 2;        // [S][BN][BK]
+  constexpr bool kBig = BN == 256;
+  static_assert(!kBig || S == 2, "the loops of 256 columns have three stages of A and two of W");
+  unsigned char *lA = smem;                                          // [S, or 3 if BN == 256][BM][BK] of two bytes
+  unsigned char *lB = lA + (kBig ? 3 : S) * BM * BK * 2;        // [S][BN][BK]
 
   // ---- tile mapping: XCD-contiguous ranges, grouped walk ----
   const int n_tiles = nM * nN;
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   // 256 x 256: an XCD runs 32 tiles at a time, 4 row-tiles x 8 column-tiles of them or 8 x 4 - the same operand bytes - but 4 is
   // 3 % faster at 24576 x 24576 x 4096 (1364 -> 1410 TFLOP/s; 3, 5, 6, 8, 16: 1-4 % slower, on some chips 6 %), and 4 % than 8
   // at 32768 x 4096 x 12288
-  constexpr int GM = BM == 256 || EPI == PRISM_EPI_RESIDUAL ? 4 : 8;
+  constexpr int GM = kBig || EPI == PRISM_EPI_RESIDUAL ? 4 : 8;
   const int group = bid / (GM * nN), first_m = group * GM;
   const int gsz = (nM - first_m) < GM ? (nM - first_m) : GM;
   const int tile_m = first_m + (bid % (GM * nN)) % gsz, tile_n = (bid % (GM * nN)) / gsz;
@@ -128,12 +130,12 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   //      before the K loop where registers are left (tiles below 256; the big tile spills).  The same for what the q/k/v
   //      epilogue reads by row: a small tile's loop is a few microseconds, and each dependent load behind it about one.
   //      (28 layers of the 0.6B shape on 391 rows, with the same in the RMSNorm: 2749 -> 2687 us.)
-  constexpr bool kEarly = BM < 256;
+  constexpr bool kEarly = !kBig;
   constexpr bool kF32Out = EPI == PRISM_EPI_RESIDUAL || EPI == PRISM_EPI_STORE_F32;
   constexpr int ES = kF32Out ? 4 : 2;                               // bytes per output element
   constexpr int OUTW = EPI == PRISM_EPI_SWIGLU ? WNT / 2 : WNT;    // output columns of the wave
   constexpr int RB = OUTW * ES, CPR = RB / 16;                      // bytes / 16-byte chunks per staged row
-  constexpr int BR = WMT < 32 ? WMT : 32, RPB = BR / 16;            // rows of a block, of those in a lane
+  constexpr int BR = WMT % 32 ? 16 : 32, RPB = BR / 16;             // rows of a block, of those in a lane
   constexpr int NBLK = WMT / BR;                                    // blocks of the wave
   constexpr int NR = 1024 / RB < BR ? 1024 / RB : BR, NI = BR / NR; // rows per instruction, instructions per block
   // lane -> (row within an instruction, chunk); 16 rows of 16 16-bit columns are less than an instruction moves: half the lanes idle
@@ -156,13 +158,18 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   const int rows_left = M - m0 - wm * WMT;                          // of the wave's rows inside the matrix
   const int64_t out_step = NR * out_pitch;
   const unsigned char *old_at = out_w;                              // steps along with the loads
-  // (whole: every row is inside the matrix, no guard per access)
-  auto load_old = [&](int i, auto whole) __attribute__((always_inline)) {
+  const int cols_left = F - (n0 + wn * OUTW + f_chunk * (16 / ES)); // of the output's columns from the lane's chunk on
+  // (whole: every row is inside the matrix, no guard per access; ragged: columns may not be, 8-bit products)
+  auto load_old = [&](int i, auto whole, auto ragged) __attribute__((always_inline)) {
     if constexpr (EPI == PRISM_EPI_RESIDUAL) {
 #pragma unroll
       for (int rr = 0; rr < NI; ++rr) {
         const int r = i * BR + rr * NR;
-        if (whole || r + f_row < rows_left) old[i & 1][rr] = __builtin_nontemporal_load(reinterpret_cast<const OutF4 *>(old_at + f_off));
+        if (ragged && cols_left < 4) {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (r + f_row < rows_left && e < cols_left) old[i & 1][rr][e] = *reinterpret_cast<const float *>(old_at + f_off + e * 4);
+        } else if (whole || r + f_row < rows_left) old[i & 1][rr] = __builtin_nontemporal_load(reinterpret_cast<const OutF4 *>(old_at + f_off));
         old_at += out_step;
       }
     }
@@ -199,7 +206,8 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   }
   if constexpr (kEarly) {
     if constexpr (kHeads) load_rows();
-    else if (full_n) load_old(0, std::false_type{});
+    else if (full_n) load_old(0, std::false_type{}, std::false_type{});
+    else if constexpr (kQ8) load_old(0, std::false_type{}, std::true_type{});
   }
 
   // ---- epilogue.  The W fragment was the instruction's first operand, so the 16 x 16 accumulator tile (i, j) is transposed:
@@ -261,12 +269,21 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   };
   // Flushes the staged block i of the wave's rows to a row-major destination (wave-uniform address of the wave's first row and
   // column, row pitch, the lane's offset).
-  auto flush_store = [&](unsigned char *dst, int64_t pitch, unsigned off, int i) __attribute__((always_inline)) {
+  auto flush_store = [&](unsigned char *dst, int64_t pitch, unsigned off, int i, auto ragged) __attribute__((always_inline)) {
     dst += (int64_t)i * BR * pitch;
 #pragma unroll
     for (int rr = 0; rr < NI; ++rr) {
       const uint4 v = staged(rr);
-      if (f_on && i * BR + rr * NR + f_row < rows_left) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<Out16 *>(dst + off));
+      if (ragged && cols_left < 16 / ES) {
+        const u32x4_t w = __builtin_bit_cast(u32x4_t, v);
+        if (f_on && i * BR + rr * NR + f_row < rows_left)
+#pragma unroll
+          for (int e = 0; e < 16 / ES - 1; ++e)
+            if (e < cols_left) {
+              if constexpr (ES == 4) *reinterpret_cast<unsigned *>(dst + off + e * 4) = w[e];
+              else *reinterpret_cast<unsigned short *>(dst + off + e * 2) = (unsigned short)(w[e / 2] >> e % 2 * 16);
+            }
+      } else if (f_on && i * BR + rr * NR + f_row < rows_left) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<Out16 *>(dst + off));
       dst += NR * pitch;
     }
   };
@@ -356,7 +373,7 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
             put16(h * 16 + e_row, j * 16 + e_col, lo);
             put16(h * 16 + e_row, j * 16 + e_col + 64, hi);
           }
-        flush_store(qk_w, pitch, qk_off, b);
+        flush_store(qk_w, pitch, qk_off, b, std::false_type{});
       }
     } else {
       // v head: rounded to the operand type, stored as half, transposed (16 consecutive tokens of one d are contiguous)
@@ -374,16 +391,16 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
     return;
   }
 
-  if (EPI == PRISM_EPI_RESIDUAL && full_n) {
+  if (EPI == PRISM_EPI_RESIDUAL && (kQ8 || full_n)) {
     // read-modify-write of the fp32 stream, whole lines per instruction; the loads of the next block are requested
     // before this block is staged, so the tile pays the memory latency once, not per block
-    auto residual = [&](auto whole) __attribute__((always_inline)) {
-      if constexpr (!kEarly) load_old(0, whole);
+    auto residual = [&](auto whole, auto ragged) __attribute__((always_inline)) {
+      if constexpr (!kEarly) load_old(0, whole, ragged);
       int64_t new_at = 0;
       asm volatile("" : "+s"(new_at));       // a chain of its own: 64 addresses shared with the loads would not fit the scalar registers
 #pragma unroll
       for (int b = 0; b < NBLK; ++b) {
-        if (b + 1 < NBLK) load_old(b + 1, whole);
+        if (b + 1 < NBLK) load_old(b + 1, whole, ragged);
 #pragma unroll
         for (int h = 0; h < RPB; ++h)
 #pragma unroll
@@ -399,16 +416,21 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
           const uint4 u = staged(rr);
           f32x4 v = old[b & 1][rr];
           v[0] += __uint_as_float(u.x); v[1] += __uint_as_float(u.y); v[2] += __uint_as_float(u.z); v[3] += __uint_as_float(u.w);
-          if (whole || r + f_row < rows_left) __builtin_nontemporal_store(v, reinterpret_cast<OutF4 *>(out_w + new_at + f_off));
+          if (ragged && cols_left < 4) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (r + f_row < rows_left && e < cols_left) *reinterpret_cast<float *>(out_w + new_at + f_off + e * 4) = v[e];
+          } else if (whole || r + f_row < rows_left) __builtin_nontemporal_store(v, reinterpret_cast<OutF4 *>(out_w + new_at + f_off));
           new_at += out_step;
         }
       }
     };
-    if (rows_left >= WMT) residual(std::true_type{});
-    else residual(std::false_type{});
+    if (kQ8 && !full_n) { if constexpr (kQ8) residual(std::false_type{}, std::true_type{}); }
+    else if (rows_left >= WMT) residual(std::true_type{}, std::false_type{});
+    else residual(std::false_type{}, std::false_type{});
     return;
   }
-  if (full_n) {
+  auto store = [&](auto ragged) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < NBLK; ++b) {
 #pragma unroll
@@ -428,13 +450,20 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
             put16(row, col, v);
           }
         }
-      flush_store(out_w, out_pitch, f_off, b);
+      flush_store(out_w, out_pitch, f_off, b, ragged);
     }
+  };
+  if (full_n) {
+    store(std::false_type{});
+    return;
+  }
+  if constexpr (kQ8) {
+    store(std::true_type{});
     return;
   }
 
   // ---- ragged last column tile (N not a multiple of the tile, or rows not 16-byte aligned): element by element
-  if constexpr (!kHeads) {
+  if constexpr (!kHeads && !kQ8) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -461,12 +490,23 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   // wave w's load instruction j fills tile rows (w * ITERS + j) * 8 .. + 8 of an operand (1 KiB of LDS)
   const unsigned ldsA_w = __builtin_amdgcn_readfirstlane(ldsA + (unsigned)wave * A_ITERS * 8 * BK * 2);
   const unsigned ldsB_w = __builtin_amdgcn_readfirstlane(ldsB + (unsigned)wave * B_ITERS * 8 * BK * 2);
-  const uint64_t baseA = (uint64_t)(uintptr_t)A + (uint64_t)m0 * rowA - kBias, baseB = (uint64_t)(uintptr_t)W + (uint64_t)n0 * rowB - kBias;
+  uint64_t baseA = (uint64_t)(uintptr_t)A + (uint64_t)m0 * rowA - kBias, baseB = (uint64_t)(uintptr_t)W + (uint64_t)n0 * rowB - kBias;
+  int to_end = nk, back = 0;                                         // slices to the row's end from where the loop begins; its step there
+  if constexpr (kQ8) {
+    const unsigned first = (unsigned)tile_n * qe.turn % (unsigned)nk;
+    baseA += first * 128u;
+    baseB += first * 128u;
+    to_end = nk - (int)first;
+    back = 128 - nk * 128;
+  }
   // the upper half of the wave's columns: SwiGLU's are the up rows, half a tile further (the swizzle repeats every 16 rows)
   const unsigned aB1 = aB0 + (unsigned)((EPI == PRISM_EPI_SWIGLU ? BN / 2 : WNT / 2) * BK) * 2u;
 #define PRISM_ACC1 "={a[0:15]}"(acc[0])
 #define PRISM_ACC2 PRISM_ACC1, "={a[16:31]}"(acc[1])
 #define PRISM_ACC4 PRISM_ACC2, "={a[32:47]}"(acc[2]), "={a[48:63]}"(acc[3])
+#define PRISM_ACC8 PRISM_ACC4, "={a[64:79]}"(acc[4]), "={a[80:95]}"(acc[5]), "={a[96:111]}"(acc[6]), "={a[112:127]}"(acc[7])
+#define PRISM_ACC10 PRISM_ACC8, "={a[128:143]}"(acc[8]), "={a[144:159]}"(acc[9])
+#define PRISM_ACC12 PRISM_ACC10, "={a[160:175]}"(acc[10]), "={a[176:191]}"(acc[11])
 #define PRISM_ACC16                                                                                                               \
   PRISM_ACC4, "={a[64:79]}"(acc[4]), "={a[80:95]}"(acc[5]), "={a[96:111]}"(acc[6]), "={a[112:127]}"(acc[7]),                        \
       "={a[128:143]}"(acc[8]), "={a[144:159]}"(acc[9]), "={a[160:175]}"(acc[10]), "={a[176:191]}"(acc[11]), "={a[192:207]}"(acc[12]), \
@@ -477,20 +517,27 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   asm volatile(LOOP : __VA_ARGS__                                                                                              \
                : [aa] "v"(aA0), [ab] "v"(aB0), [ab2] "v"(aB1), PRISM_AB(0), PRISM_AB(1), PRISM_AB(2), PRISM_AB(3), PRISM_AB(4), \
                  PRISM_AB(5), PRISM_AB(6), PRISM_AB(7), [la] "s"(ldsA_w), [lb] "s"(ldsB_w), [pa] "s"(baseA), [pb] "s"(baseB),   \
-                 [nk] "s"(nk)                                                                                                  \
+                 [nk] "s"(nk), [bk] "s"(back), [wr] "s"(to_end)                                                                \
                : CLOBBERS)
+#define PRISM_RUN_Q8(NAME, LIKE, ...) PRISM_RUN_TY(PRISM_KLOOP_Q8_##NAME, PRISM_KLOOP_Q8_CLOBBERS_##LIKE, __VA_ARGS__)
+#define PRISM_RUN_16(NAME, ...)                                                                                                 \
+  do {                                                                                                                         \
+    if constexpr (Mfma<OT>::kIsF16) PRISM_RUN_TY(PRISM_KLOOP_##NAME("f16"), PRISM_KLOOP_CLOBBERS_##NAME, __VA_ARGS__);          \
+    else PRISM_RUN_TY(PRISM_KLOOP_##NAME("bf16"), PRISM_KLOOP_CLOBBERS_##NAME, __VA_ARGS__);                                    \
+  } while (0)
 #define PRISM_RUN(NAME, ...)                                                                                                    \
   do {                                                                                                                         \
-    if constexpr (kQ8) PRISM_RUN_TY(PRISM_KLOOP_##NAME("i32_16x16x64_i8"), PRISM_KLOOP_CLOBBERS_##NAME, __VA_ARGS__);           \
-    else if constexpr (Mfma<OT>::kIsF16) PRISM_RUN_TY(PRISM_KLOOP_##NAME("f32_16x16x32_f16"), PRISM_KLOOP_CLOBBERS_##NAME, __VA_ARGS__); \
-    else PRISM_RUN_TY(PRISM_KLOOP_##NAME("f32_16x16x32_bf16"), PRISM_KLOOP_CLOBBERS_##NAME, __VA_ARGS__);                       \
+    if constexpr (kQ8) PRISM_RUN_Q8(NAME, NAME, __VA_ARGS__);                                                                   \
+    else PRISM_RUN_16(NAME, __VA_ARGS__);                                                                                       \
   } while (0)
   if constexpr (BM == 256) PRISM_RUN(256, PRISM_ACC16);
-  else if constexpr (kHeads && BM == 64 && S == 6) PRISM_RUN(64x128_6_HEAD, PRISM_ACC2);
-  else if constexpr (kHeads && BM == 64) PRISM_RUN(64x128_3_HEAD, PRISM_ACC2);
-  else if constexpr (kHeads && S == 5) PRISM_RUN(128x128_5_HEAD, PRISM_ACC4);
-  else if constexpr (kHeads && S == 3) PRISM_RUN(128x128_3_HEAD, PRISM_ACC4);
-  else if constexpr (kHeads) PRISM_RUN(128x128_2_HEAD, PRISM_ACC4);
+  else if constexpr (kBig && BM == 192) PRISM_RUN_Q8(192, 256, PRISM_ACC12);
+  else if constexpr (kBig) PRISM_RUN_Q8(160, 256, PRISM_ACC10);
+  else if constexpr (kHeads && BM == 64 && S == 6) PRISM_RUN_16(64x128_6_HEAD, PRISM_ACC2);
+  else if constexpr (kHeads && BM == 64) PRISM_RUN_16(64x128_3_HEAD, PRISM_ACC2);
+  else if constexpr (kHeads && S == 5) PRISM_RUN_16(128x128_5_HEAD, PRISM_ACC4);
+  else if constexpr (kHeads && S == 3) PRISM_RUN_16(128x128_3_HEAD, PRISM_ACC4);
+  else if constexpr (kHeads) PRISM_RUN_16(128x128_2_HEAD, PRISM_ACC4);
   else if constexpr (BM == 32 && BN == 32) PRISM_RUN(32x32_9, PRISM_ACC1);
   else if constexpr (BM == 64 && BN == 32) PRISM_RUN(64x32_7, PRISM_ACC1);
   else if constexpr (BM == 32 && BN == 64) PRISM_RUN(32x64_4, PRISM_ACC2);
@@ -498,9 +545,11 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   else if constexpr (BM == 128 && BN == 64 && S == 6) PRISM_RUN(128x64_6, PRISM_ACC2);
   else if constexpr (BM == 128 && BN == 64) PRISM_RUN(128x64_3, PRISM_ACC2);
   else if constexpr (S == 5) PRISM_RUN(128x128_5, PRISM_ACC4);
-  else if constexpr (S == 4) PRISM_RUN(128x128_4, PRISM_ACC4);
+  else if constexpr (S == 4) PRISM_RUN_16(128x128_4, PRISM_ACC4);
   else PRISM_RUN(128x128_2, PRISM_ACC4);
 #undef PRISM_RUN
+#undef PRISM_RUN_16
+#undef PRISM_RUN_Q8
 #undef PRISM_RUN_TY
 #undef PRISM_AB
   epilogue();

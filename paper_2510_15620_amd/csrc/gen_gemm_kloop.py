@@ -1,10 +1,12 @@
 #!/usr/bin/env python3
-"""Generates gemm_16_kloop.inc: the hand-scheduled K loops of the GEMM tiles.
+"""Generates gemm_16_kloop.inc and gemm_q8_kloop.inc: the hand-scheduled K loops of the GEMM tiles.
 
-    python gen_gemm_kloop.py > gemm_16_kloop.inc        (the output is committed too)
+    python gen_gemm_kloop.py > gemm_16_kloop.inc        (the outputs are committed too)
+    python gen_gemm_kloop.py q8 > gemm_q8_kloop.inc
 
-A loop sees bytes: slices of 128 bytes a row, fragments of 16 bytes a lane.  The matrix instruction is its parameter: 16x16x32 on 16-bit
-values or 16x16x64 on 8-bit integers, which take the same registers and cycles; below, k counts 16-bit values.
+A loop sees bytes: slices of 128 bytes a row, fragments of 16 bytes a lane.  The loops on 8-bit integers differ from those on 16-bit values in
+the matrix instruction, 16x16x64 for 16x16x32 from the same registers in the same cycles, in that they may begin anywhere in K and go round (rotated,
+below), integers being exact in any order, and in the large tiles of fewer rows.  Elsewhere in this file k counts 16-bit values.
 
 The 256x256x64 tile.  4 wavefronts (one per SIMD, so each owns 512 registers), wave grid 2x2, wave tile 128x128 = 8x8
 accumulator tiles of v_mfma_f32_16x16x32 kept in 256 AGPRs: the largest wave tile the register file allows, i.e. the
@@ -35,6 +37,11 @@ free of branches.  The stage offsets are immediates, so the loop is unrolled ove
 The W fragment is the first MFMA operand, so accumulator tiles come out transposed (a lane owns one row of A).
 """
 import math
+import sys
+
+Q8 = sys.argv[1:] == ["q8"]
+PREFIX, CLOBBERS = ("PRISM_KLOOP_Q8", "PRISM_KLOOP_Q8_CLOBBERS") if Q8 else ("PRISM_KLOOP", "PRISM_KLOOP_CLOBBERS")
+MFMA = "v_mfma_i32_16x16x64_i8" if Q8 else 'v_mfma_f32_16x16x32_" TY "'
 
 # ---- register plan (all clobbered) ----
 AA, AA2, AB, AB2 = [116, 117], [118, 119], [120, 121], [122, 123]   # LDS address of the lane's first fragment row, per step: A stages
@@ -46,7 +53,9 @@ CLOBBER_S = list(range(20, 30))
 STAGE = 32768                           # bytes per LDS stage of one operand
 A_STAGES, B_STAGES, PERIOD = 3, 2, 6
 TILE_ROWS = 2048                        # 16 rows x 128 B
-RSTRIDE, PB, LSTRIDE = 3, 56, 6
+# 256 columns by 32 TM rows: accumulator tiles of a wave by rows, RSTRIDE, PB, LSTRIDE
+BIG = {256: (8, 3, 56, 6), 192: (6, 3, 42, 6), 160: (5, 2, 34, 5)}
+TM, RSTRIDE, PB, LSTRIDE = BIG[256]
 
 
 def v4(r):
@@ -59,16 +68,16 @@ def acc(i, j):
 
 
 def reads(fs, k, t):
-    """The 16 fragment reads of step k of slice t into fragment set fs, in the order of their first use."""
+    """The fragment reads of step k of slice t into fragment set fs, in the order of their first use."""
     sa, sb = t % A_STAGES, t % B_STAGES
-    base, off = (AA2, 0) if sa == 2 else (AA, sa * STAGE)              # a read's immediate offset ends at 64 KiB
+    base, off = (AA2, 0) if sa == 2 else (AA, sa * TM * 4096)          # a read's immediate offset ends at 64 KiB
     ra = lambda i: f"ds_read_b128 {v4(F[fs]['A'][i])}, v{base[k]} offset:{off + i * TILE_ROWS}"
     rb = lambda j: f"ds_read_b128 {v4(F[fs]['B'][j])}, v{(AB if j < 4 else AB2)[k]} offset:{sb * STAGE + j % 4 * TILE_ROWS}"
-    return [ra(0), rb(0), ra(1)] + [rb(j) for j in range(1, 8)] + [ra(i) for i in range(2, 8)]
+    return [ra(0), rb(0), ra(1)] + [rb(j) for j in range(1, 8)] + [ra(i) for i in range(2, TM)]
 
 
 def mfma(fs, i, j):
-    return f'v_mfma_" TY " {acc(i, j)}, {v4(F[fs]["B"][j])}, {v4(F[fs]["A"][i])}, {acc(i, j)}'
+    return f'{MFMA} {acc(i, j)}, {v4(F[fs]["B"][j])}, {v4(F[fs]["A"][i])}, {acc(i, j)}'
 
 
 def load_group(which, n, lds_off, m0_at=0):
@@ -80,14 +89,25 @@ def load_group(which, n, lds_off, m0_at=0):
     return [f"{m0(j)}global_load_lds_dwordx4 %[{off}{j}], {base} offset:{j % 4 * 1024}" for j in range(n)]
 
 
-def loads(which, stage):
-    return load_group(which, 8, stage * STAGE)
+def loads(which, stage, m0_at=0):
+    return load_group(which, TM, stage * TM * 4096, m0_at) if which == "A" else load_group(which, 8, stage * STAGE, m0_at)
+
+
+def rotated(wraps, exists, step, high):
+    """The bytes to the next slice, in step and high: 128, where the slice is the row's last back to its first ([bk] = 128 - the row's bytes), and none
+    where no next slice is wanted (scc then says whether one is).  Launches of few rows, whose tiles would all read the same k of rows that are a power of two
+    apart, and with them the same few memory channels, begin at different slices."""
+    return [wraps, f"s_cselect_b32 {step}, %[bk], 128", f"s_ashr_i32 {high}, {step}, 31", exists, f"s_cselect_b32 {step}, {step}, 0",
+            f"s_cselect_b32 {high}, {high}, 0"]
 
 
 def advance(which):
     """Moves one operand's base to the next slice while that stays inside the operand (s25 / s29 = index of the slice the
     base points at, s26 = last slice)."""
     idx, lo, hi = ("s25", "s20", "s21") if which == "A" else ("s29", "s22", "s23")
+    if Q8:
+        return rotated(f"s_cmp_eq_u32 {idx}, s31", f"s_cmp_lt_u32 {idx}, s26", "s27", "s30") + \
+            ["s_cselect_b32 s28, 1, 0", f"s_add_u32 {lo}, {lo}, s27", f"s_addc_u32 {hi}, {hi}, s30", f"s_add_u32 {idx}, {idx}, s28"]
     return [f"s_cmp_lt_u32 {idx}, s26", "s_cselect_b32 s27, 128, 0", "s_cselect_b32 s28, 1, 0",
             f"s_add_u32 {lo}, {lo}, s27", f"s_addc_u32 {hi}, {hi}, 0", f"s_add_u32 {idx}, {idx}, s28"]
 
@@ -96,33 +116,36 @@ def mfma_order():
     """Two rows of accumulator tiles at a time, column by column, turning at the ends: consecutive MFMAs differ in one operand
     fragment (fewer operand bits toggle; 0.8 % faster than row by row)."""
     out = []
-    for p in range(4):
+    for p in range((TM + 1) // 2):
         for n, j in enumerate(range(8) if p % 2 == 0 else range(7, -1, -1)):
-            out += [(2 * p + i, j) for i in ((0, 1) if n % 2 == 0 else (1, 0))]
+            out += [(2 * p + i, j) for i in ((0, 1) if n % 2 == 0 else (1, 0)) if 2 * p + i < TM]
     return out
 
 
 def slice_body(t):
+    step, whole, n = 8 * TM, 16 * TM, TM + 8            # MFMAs of a step and of the slice; fragment reads of a step, loads of the slice
     behind = {}                                         # position -> what is issued behind that MFMA
-    for n, r in enumerate(reads(1, 1, t)):
-        behind.setdefault(n * RSTRIDE, []).append(r)
-    for n, r in enumerate(reads(0, 0, t + 1)):
-        behind.setdefault(64 + n * RSTRIDE, []).append(r)
+    for i, r in enumerate(reads(1, 1, t)):
+        behind.setdefault(i * RSTRIDE, []).append(r)
+    for i, r in enumerate(reads(0, 0, t + 1)):
+        behind.setdefault(step + i * RSTRIDE, []).append(r)
     # the loads requested behind this slice's barrier, and those of the slice before that reach into this one (they go to the
-    # stages that were freed by its barrier)
-    for s, shift in ((t, 0), (t - 1, 128)):
-        for n, l in enumerate(loads("B", s % B_STAGES) + loads("A", s % A_STAGES)):
-            p = PB + 1 + n * LSTRIDE - shift
-            if 0 <= p < 128 and (shift == 0 or p < PB):
-                behind.setdefault(p, []).append(l)
-    assert 15 * RSTRIDE < PB and PB + 1 + 15 * LSTRIDE - 128 < PB
+    # stages that were freed by its barrier; the first turn repeats the youngest there, so the first of them sets M0 itself)
+    at = [PB + 1 + i * LSTRIDE for i in range(n)]
+    tail = next((i for i in range(n) if at[i] >= whole), n)
+    assert tail >= 8
+    for p, l in zip(at[:tail], loads("B", t % B_STAGES) + loads("A", t % A_STAGES)):
+        behind.setdefault(p, []).append(l)
+    for p, l in zip(at[tail:], loads("A", (t - 1) % A_STAGES, tail - 8)[tail - 8:]):
+        behind.setdefault(p - whole, []).append(l)
+    assert (n - 1) * RSTRIDE < PB < step and at[-1] - whole < PB
     out = []
-    for m in range(128):
-        if m in (0, 64):
-            out.append("s_waitcnt lgkmcnt(0)")          # the step's fragments; the last was requested 18 MFMAs ago
+    for m in range(whole):
+        if m in (0, step):
+            out.append("s_waitcnt lgkmcnt(0)")          # the step's fragments; of 256 rows the last was requested 18 MFMAs ago
         if m == PB:
-            out += ["s_waitcnt vmcnt(8) lgkmcnt(0)"] + advance("A") + advance("B") + ["s_barrier"]
-        out.append(mfma(m // 64, *mfma_order()[m % 64]))
+            out += [f"s_waitcnt vmcnt({TM}) lgkmcnt(0)"] + advance("A") + advance("B") + ["s_barrier"]
+        out.append(mfma(m // step, *mfma_order()[m % step]))
         out += behind.get(m, [])
     return out
 
@@ -131,13 +154,13 @@ def kloop():
     s = []
     for k in range(2):                                  # the steps' addresses differ only in a swizzled chunk bit
         s += [f"v_xor_b32 v{r[k]}, {64 * k}, %[{a}]" for r, a in ((AA, "aa"), (AB, "ab"), (AB2, "ab2"))]
-        s += [f"v_add_u32 v{AA2[k]}, {2 * STAGE}, v{AA[k]}"]
+        s += [f"v_add_u32 v{AA2[k]}, {2 * TM * 4096}, v{AA[k]}"]
     s += ["s_mov_b64 s[20:21], %[pa]", "s_mov_b64 s[22:23], %[pb]", "s_mov_b32 s24, %[nk]", "s_sub_u32 s26, %[nk], 1",
-          "s_mov_b32 s25, 0", "s_mov_b32 s29, 0"]
+          "s_mov_b32 s25, 0", "s_mov_b32 s29, 0"] + (["s_sub_u32 s31, %[wr], 1"] if Q8 else [])
     # ---- prologue: B and A of slices 0 and 1, A of slice 2; the accumulators are cleared while the first of them arrive
     s += loads("B", 0) + advance("B") + loads("A", 0) + advance("A") + loads("B", 1) + loads("A", 1) + advance("A") + loads("A", 2)
-    s += [f"v_accvgpr_write_b32 a{r}, 0" for r in range(256)]
-    s += ["s_waitcnt vmcnt(24)", "s_barrier"] + reads(0, 0, 0)
+    s += [f"v_accvgpr_write_b32 a{r}, 0" for r in range(32 * TM)]
+    s += [f"s_waitcnt vmcnt({8 + 2 * TM})", "s_barrier"] + reads(0, 0, 0)
     s += ["L_loop_%=:"]
     for t in range(PERIOD):
         s += slice_body(t) + ["s_sub_u32 s24, s24, 1", "s_cmp_eq_u32 s24, 0"]
@@ -216,6 +239,9 @@ class Small:
     def advance(self, exists):
         """Both bases to the next slice if that exists: near the end the loads re-read the last slice, in bounds, into stages
         that nobody reads any more."""
+        if Q8:
+            return ["s_sub_u32 s26, s26, 1"] + rotated("s_cmp_eq_u32 s26, 0", exists, "s25", "s27") + \
+                ["s_add_u32 s20, s20, s25", "s_addc_u32 s21, s21, s27", "s_add_u32 s22, s22, s25", "s_addc_u32 s23, s23, s27"]
         return [exists, "s_cselect_b32 s25, 128, 0", "s_add_u32 s20, s20, s25", "s_addc_u32 s21, s21, 0", "s_add_u32 s22, s22, s25",
                 "s_addc_u32 s23, s23, 0"]
 
@@ -228,6 +254,7 @@ class Small:
                 if self.high:
                     s.append(f"v_add_u32 v{self.addr(which, k, True)}, 65536, v{self.addr(which, k, False)}")
         s += ["s_mov_b64 s[20:21], %[pa]", "s_mov_b64 s[22:23], %[pb]", "s_sub_u32 s24, %[nk], 1"]    # s24: slices after this one
+        s += ["s_mov_b32 s26, %[wr]"] if Q8 else []
         n_pro = S if RA == 1 else S - 1
         for t in range(n_pro):
             s += self.loads(t) + (self.advance(f"s_cmp_gt_u32 s24, {t}") if t + 1 < n_pro else [])
@@ -263,16 +290,16 @@ class Small:
                     s += [f"s_waitcnt {outstanding}"]
                 (i, j), u = order[m % NS], 2 * t + m // NS
                 r = (i * self.TN + j) * 4
-                s.append(f'v_mfma_" TY " a[{r}:{r + 3}], {self.frag(u, "B", j)}, {self.frag(u, "A", i)}, a[{r}:{r + 3}]')
+                s.append(f'{MFMA} a[{r}:{r + 3}], {self.frag(u, "B", j)}, {self.frag(u, "A", i)}, a[{r}:{r + 3}]')
                 s += behind.get(m, [])
             s += ["s_sub_u32 s24, s24, 1"] + (["s_cbranch_scc1 L_done_%="] if t + 1 < period else ["s_cbranch_scc0 L_loop_%="])
         s += ["L_done_%=:", "s_waitcnt vmcnt(0) lgkmcnt(0)", "s_nop 15", "s_nop 15"]
         return s
 
     def emit(self):
-        emit(f"PRISM_KLOOP_{self.name}(TY)", self.text())
-        regs = ", ".join(f'"v{r}"' for r in range(FIRST_V, self.last_v + 1)) + ", " + ", ".join(f'"s{r}"' for r in range(20, 26))
-        print(f"#define PRISM_KLOOP_CLOBBERS_{self.name} {regs}, \"scc\", \"memory\"")
+        emit(f"{PREFIX}_{self.name}" + ("" if Q8 else "(TY)"), self.text())
+        regs = ", ".join(f'"v{r}"' for r in range(FIRST_V, self.last_v + 1)) + ", " + ", ".join(f'"s{r}"' for r in range(20, 28 if Q8 else 26))
+        print(f"#define {CLOBBERS}_{self.name} {regs}, \"scc\", \"memory\"")
         print()
 
 
@@ -306,19 +333,26 @@ def emit(name, lines):
 
 
 def main():
+    global TM, RSTRIDE, PB, LSTRIDE
     print("// Generated by gen_gemm_kloop.py - do not edit.  See that file for the schedule.")
-    print("// PRISM_KLOOP_<tile>(TY), TY = \"f32_16x16x32_f16\", \"f32_16x16x32_bf16\" or \"i32_16x16x64_i8\": accumulators a[0:...], tile (i, j) of 16 x 16 in the four from 4 (TN i + j) on;")
-    print("// aa / ab / ab2 LDS byte address of the lane's first fragment row of A, of the lower and of the upper half of the wave's B columns")
-    print("// (step 0, stage 0); ga / gb byte offset from pa / pb of the chunk this lane fetches in each of its wave's load instructions,")
-    print("// less 1024 (j % 4); la / lb LDS byte address of the first row the first of them fills (stage 0, uniform); nk number of slices.")
+    if Q8:
+        print("// PRISM_KLOOP_Q8_<tile>: as PRISM_KLOOP_<tile>, sums of 8-bit integers; bk = 128 - a row's bytes, wr slices from where pa / pb point to the row's end.")
+    else:
+        print("// PRISM_KLOOP_<tile>(TY), TY = \"f16\" or \"bf16\": accumulators a[0:...], tile (i, j) of 16 x 16 in the four from 4 (TN i + j) on;")
+        print("// aa / ab / ab2 LDS byte address of the lane's first fragment row of A, of the lower and of the upper half of the wave's B columns")
+        print("// (step 0, stage 0); ga / gb byte offset from pa / pb of the chunk this lane fetches in each of its wave's load instructions,")
+        print("// less 1024 (j % 4); la / lb LDS byte address of the first row the first of them fills (stage 0, uniform); nk number of slices.")
     print()
-    emit("PRISM_KLOOP_256(TY)", kloop())
-    regs = ", ".join(f'"v{r}"' for r in CLOBBER_V) + ", " + ", ".join(f'"s{r}"' for r in CLOBBER_S)
+    for rows in BIG if Q8 else [256]:
+        TM, RSTRIDE, PB, LSTRIDE = BIG[rows]
+        emit(f"{PREFIX}_{rows}" + ("" if Q8 else "(TY)"), kloop())
+    regs = ", ".join(f'"v{r}"' for r in CLOBBER_V) + ", " + ", ".join(f'"s{r}"' for r in CLOBBER_S + ([30, 31] if Q8 else []))
     for c in SMALL:
-        c.emit()
+        if not (Q8 and (c.name.endswith("HEAD") or c.name == "128x128_4")):
+            c.emit()
     # m0 (written before the direct-to-LDS loads) is not listed: the compiler reserves it, sets it right before each of
     # its own uses and never keeps a value in it across a statement; hipcc diagnoses it in a clobber list
-    print(f"#define PRISM_KLOOP_CLOBBERS_256 {regs}, \"scc\", \"memory\"")
+    print(f"#define {CLOBBERS}_256 {regs}, \"scc\", \"memory\"")
 
 
 if __name__ == "__main__":

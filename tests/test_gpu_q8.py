@@ -274,7 +274,8 @@ def run_product(M, N, K, epilogue, dtype, seed=0):
 
 SIZES = [(1, 2, 1), (1, 64, 64), (1, 4096, 256), (2, 66, 129), (3, 1000, 500), (7, 130, 1003), (17, 48, 128), (24, 514, 4096), (33, 2560, 640), (64, 62, 12288), (65, 4096, 384),
          (100, 1026, 257), (129, 6144, 1024), (200, 2000, 2047), (391, 4096, 1024), (513, 258, 320), (777, 2562, 1003), (1154, 2560, 512), (2000, 130, 96),
-         (3000, 1024, 640), (4100, 6144, 640), (5000, 1234, 333)]
+         (3000, 1024, 640), (4100, 6144, 640), (5000, 1234, 333),
+         (18, 17076, 785), (517, 20142, 66), (130, 5648, 2565), (17207, 68, 1040), (517, 20866, 141)]         # tests/test_q8_plan.py: every tile
 
 
 @pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
@@ -283,13 +284,30 @@ def test_gemm(M, N, K, epilogue, dtype):
     run_product(M, N, K, epilogue, dtype)
 
 
+ODD_SIZES = [(5, 31, 40), (300, 257, 70), (1543, 2501, 1003), (2600, 1281, 130)]
+
+
 @pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
 def test_gemm_odd_widths(epilogue, dtype):
     """Outputs whose rows begin at no multiple of anything, and last tiles of a single column."""
-    for M, N, K in ((5, 31, 40), (300, 257, 70), (1543, 2501, 1003), (2600, 1281, 130)):
+    for M, N, K in ODD_SIZES:
         if epilogue == B.EPI_SWIGLU:
             N *= 2
         run_product(M, N, K, epilogue, dtype)
+
+
+@pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
+def test_gemm_that_begins_anywhere_in_k(epilogue, dtype):
+    """Up to 512 rows by weights whose rows are a multiple of 4 KiB apart: column tiles begin at different slices of K and come round."""
+    for M, N, K in ((70, 1026, 4096), (300, 2048, 4000), (512, 514, 8192), (200, 260, 12288), (40, 24576, 4096)):
+        run_product(M, N, K, epilogue, dtype)
+
+
+@pytest.mark.parametrize("M", [1, 8, 9, 16, 17, 32, 33, 64, 65])
+def test_gemm_around_the_kernel_of_few_rows(M):
+    for N, K in ((64, 70), (4096, 1024), (4098, 1024), (8192, 1024), (8194, 1000), (2046, 2176), (2048, 2176), (512, 4224)):
+        run_product(M, N, K, B.EPI_RESIDUAL, F32)
+        run_product(M, N, K, B.EPI_SWIGLU, F16)
 
 
 @pytest.mark.parametrize("M,N", [(1, 64), (130, 300)])
