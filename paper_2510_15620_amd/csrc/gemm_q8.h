@@ -14,15 +14,24 @@ struct Q8Operands {
   int turn;
 };
 
-// silu(g) * u in fp32, rounded to 16 bits by its callers.  The division is correctly rounded: a product with the reciprocal
-// instruction takes half of this epilogue's arithmetic away (13.8 -> 9.2 thousand cycles of a 256 x 256 tile) and no time where the
-// chip is full and at its power limit (24576 x 24576 x 4096: 3350 us, with the division 3337), but is off by
-// an ulp more and returns 0 where 1 + e^-g exceeds 2^126, values that bf16 still holds.
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+// silu(g) * u of the 8-bit products, off by 6.5 + 1.5 |g| in 2^-24 (exponential, its argument, sum, reciprocal, two products).  Their loops are half as long
+// as the 16-bit ones, so that the epilogue is a quarter of a tile of K = 4096, and a division's ten instructions show (with the two-at-a-time rounding below, us: 11520 x 24576 x 4096
+// 895 -> 847, x 1024 355 -> 313; the rounding alone, stored 11520 x 12288 x 4096 450 -> 432).  Where 1 + e^-g
+// exceeds 2^126 the reciprocal is 0: the result is then below 10^-36 |u|.
+__device__ __forceinline__ float q8_silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
-// Results of 8-bit products in 16 bits: a NaN (of a row without a scale) stays one, which half's saturation would turn into a number
-template <typename T> __device__ __forceinline__ T q8_round(float v) { return from_f32<T>(v); }
-template <> __device__ __forceinline__ f16 q8_round<f16>(float v) { return v == v ? from_f32<f16>(v) : (f16)v; }
+// Results of 8-bit products in 16 bits: rounded to nearest, half saturated.  A NaN (of a row without a scale) stays one; gfx950's minimum and maximum of
+// three keep it, and take two values at a time.
+template <typename T> __device__ __forceinline__ auto q8_round4(const f32x4 &v) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 r = __builtin_convertvector(v, T4);
+  if constexpr (__is_same(T, f16)) {
+    constexpr f16 top = (f16)65504.0f;
+    const T4 hi = {top, top, top, top};
+    r = __builtin_elementwise_minimum(__builtin_elementwise_maximum(r, -hi), hi);
+  }
+  return r;
+}
 
 // Products of few rows, up to 64 (gemm_q8_rows.hip; arguments checked)
 int launch_gemm_q8_rows(int epilogue, const prism_q8 &a, const prism_q8 &w, int out_dtype, void *out, int64_t out_stride, hipStream_t s);

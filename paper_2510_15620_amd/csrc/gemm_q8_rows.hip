@@ -112,7 +112,7 @@ __global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, 
     if constexpr (kGlu) {
       const f32x4 up = total(i * NT + j + NO, sw[e][kGlu ? 1 : 0]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = silu_mul(y[k], up[k]);
+      for (int k = 0; k < 4; ++k) y[k] = q8_silu_mul(y[k], up[k]);
     }
     if constexpr (EPI == PRISM_EPI_RESIDUAL) y += old[e];
     if (m >= M) continue;
@@ -123,11 +123,8 @@ __global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, 
         for (int k = 0; k < 4; ++k)
           if (c + k < F) o[k] = y[k];
     } else {
-      typedef OT Quad __attribute__((ext_vector_type(4)));
-      typedef Quad Quad_any __attribute__((aligned(2)));
-      Quad v;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = q8_round<OT>(y[k]);
+      const auto v = q8_round4<OT>(y);
+      typedef decltype(q8_round4<OT>(y)) Quad_any __attribute__((aligned(2)));
       OT *o = reinterpret_cast<OT *>(out_) + m * q.ldo + c;
       if (c + 4 <= F) *reinterpret_cast<Quad_any *>(o) = v;
       else

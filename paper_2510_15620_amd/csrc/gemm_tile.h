@@ -42,6 +42,12 @@ __device__ __forceinline__ int swz(int row, int chunk) { return chunk ^ ((row >>
 #define PRISM_GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
 #define PRISM_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 
+// silu(g) * u in fp32, rounded to 16 bits by its callers.  The division is correctly rounded: a product with the reciprocal
+// instruction takes half of this epilogue's arithmetic away (13.8 -> 9.2 thousand cycles of a 256 x 256 tile) and no time where the
+// chip is full and at its power limit (24576 x 24576 x 4096: 3350 us, with the division 3337), but is off by
+// an ulp more and returns 0 where 1 + e^-g exceeds 2^126, values that bf16 still holds.
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
 // LDS bytes of a tile's operand stages
 template <int BM, int BN, int S> constexpr int stage_bytes() { return ((BN == 256 ? 3 : S) * BM + S * BN) * BK * 2; }
 
@@ -241,10 +247,6 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
       return r;
     }
   };
-  auto to16 = [&](float v) __attribute__((always_inline)) {
-    if constexpr (kQ8) return q8_round<OT>(v);
-    else return from_f32<OT>(v);
-  };
   __syncthreads();              // every wave's operand loads have landed and nobody reads operands any more
   constexpr int SWZ = CPR >= 16 ? 15 : CPR - 1;                     // chunk rotation by row: spreads a column of 16-byte
                                                                     // writes (one per row) over the banks
@@ -443,10 +445,15 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = AC(i, j, q);
             put32(row, col, v);
+          } else if constexpr (kQ8) {
+            f32x4 v;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = EPI == PRISM_EPI_SWIGLU ? q8_silu_mul(AC(i, j, q), AC(i, j + TN / 2, q)) : AC(i, j, q);
+            put16(row, col, q8_round4<OT>(v));
           } else {
             typename Mfma<OT>::vec4 v;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = to16(EPI == PRISM_EPI_SWIGLU ? silu_mul(AC(i, j, q), AC(i, j + TN / 2, q)) : AC(i, j, q));
+            for (int q = 0; q < 4; ++q) v[q] = from_f32<OT>(EPI == PRISM_EPI_SWIGLU ? silu_mul(AC(i, j, q), AC(i, j + TN / 2, q)) : AC(i, j, q));
             put16(row, col, v);
           }
         }
@@ -472,13 +479,13 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
           const int row = m0 + wm * WMT + i * 16 + e_row, col = n0 + wn * OUTW + j * 16 + e_col + q;
           if (row >= M || col >= F) continue;
           if (EPI == PRISM_EPI_SWIGLU) {
-            reinterpret_cast<OT *>(out_)[row * out_row + col] = to16(silu_mul(AC(i, j, q), AC(i, j + TN / 2, q)));
+            reinterpret_cast<OT *>(out_)[row * out_row + col] = from_f32<OT>(silu_mul(AC(i, j, q), AC(i, j + TN / 2, q)));
           } else if (EPI == PRISM_EPI_RESIDUAL) {
             reinterpret_cast<float *>(out_)[row * out_row + col] += AC(i, j, q);
           } else if (EPI == PRISM_EPI_STORE_F32) {
             reinterpret_cast<float *>(out_)[row * out_row + col] = AC(i, j, q);
           } else {
-            reinterpret_cast<OT *>(out_)[row * out_row + col] = to16(AC(i, j, q));
+            reinterpret_cast<OT *>(out_)[row * out_row + col] = from_f32<OT>(AC(i, j, q));
           }
         }
   }

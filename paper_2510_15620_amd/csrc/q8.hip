@@ -208,9 +208,11 @@ __global__ __launch_bounds__(256) void dequantize_q8_kernel(const int8_t *__rest
   T *o = out + row * out_stride;
   for (int i = (threadIdx.x % lanes) * 8; i < cols; i += lanes * 8) {
     const uint2 c = *reinterpret_cast<const uint2 *>(in + i);
-    typename Pack<T, 8>::vec v;
+    f32x4 x[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = q8_round<T>((float)(int8_t)((e < 4 ? c.x : c.y) >> (e & 3) * 8) * s);
+    for (int e = 0; e < 8; ++e) x[e / 4][e % 4] = (float)(int8_t)((e < 4 ? c.x : c.y) >> (e & 3) * 8) * s;
+    const auto lo = q8_round4<T>(x[0]), hi = q8_round4<T>(x[1]);
+    const typename Pack<T, 8>::vec v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     if (i + 8 <= cols) *reinterpret_cast<typename Pack<T, 8>::any *>(o + i) = v;
     else
       for (int e = 0; e < 8; ++e)

@@ -243,14 +243,14 @@ EPILOGUES = [(B.EPI_STORE, BF16), (B.EPI_STORE, F16), (B.EPI_STORE_F32, F32), (B
 
 
 def check_product(epilogue, dtype, out, old, y):
-    """fp32: the sum's conversion and two products, 3 u; the residual's addition one of the result.  SwiGLU: gate and up 3 u each, 1 + e, division and product 3 u, one ulp (2 u) of the
-    exponential, and the exponent g log2(e): gate's 3 u, its own product's and constant's 1.5 u, in all 4.5 u |g|.  Where the exponential leaves fp32 (|g| > 88) the result is below
-    89 e^-88 |up| = 6e-37 |up|.  16 bits: half a step more, and half the least subnormal."""
+    """fp32: the sum's conversion and two products, 3 u; the residual's addition one of the result.  SwiGLU: gate and up 3 u each, 1 + e and two products 3 u, the reciprocal and the
+    exponential an ulp (2 u) each, and the exponent g log2(e): gate's 3 u, its own product's and constant's 1.5 u, in all 4.5 u |g|.  Where 1 + e leaves the reciprocal's range
+    (2^126, |g| > 87.3) the result is 0 for what is below 88 2^-126 |up| < 1.1e-36 |up|.  16 bits: half a step more, and half the least subnormal."""
     if epilogue == B.EPI_SWIGLU:
         f = y.shape[1] // 2
         gate, up = y[:, :f], y[:, f:]
         want = gate * torch.sigmoid(gate) * up
-        err = want.abs() * (11.1 + 4.6 * gate.abs()) * U + 6e-37 * up.abs()
+        err = want.abs() * (13.1 + 4.6 * gate.abs()) * U + 1.1e-36 * up.abs()
     elif epilogue == B.EPI_RESIDUAL:
         want = old.double() + y
         err = y.abs() * 3.01 * U + want.abs() * U
