@@ -4,6 +4,8 @@
 // A row x has scale = max|x| / 127 and codes x / scale, rounded to the nearest integer, ties to even.  The norm's rows are n = x r gain with one r a row, which
 // cancels in n / scale: code = x gain 127 / max|x gain|, so the sum of squares (for r) and the maximum meet in one reduction and the row is read once.
 // All of it is bound by memory; rows stay in registers between the maximum and the codes.
+#include <type_traits>
+
 #include "gemm_q8.h"
 
 namespace prism {
@@ -15,38 +17,65 @@ template <typename T, int N> struct Pack {
   typedef T vec __attribute__((ext_vector_type(N)));
   typedef vec any __attribute__((aligned(sizeof(T))));
 };
-// values i .. i + N - 1 of a row of n, zeros behind its end
+// Values i .. i + N - 1 of a row of n, zeros behind its end.  16 (or 8) bytes that reach over the end are read from further in front and shifted down: one load,
+// where a load a value and their waits would hold up the row's other loads
 template <typename T, int N> __device__ __forceinline__ typename Pack<T, N>::vec load_row(const T *row, int i, int n) {
-  typename Pack<T, N>::vec v = {};
+  typedef typename Pack<T, N>::vec vec;
+  vec v = {};
   if (i + N <= n) v = *reinterpret_cast<const typename Pack<T, N>::any *>(row + i);
-  else
-    for (int e = 0; e < N; ++e)
-      if (i + e < n) v[e] = row[i + e];
+  else if (i < n) {
+    if (n >= N) {
+      typedef std::conditional_t<sizeof(vec) == 16, unsigned __int128, unsigned long long> bits;
+      v = *reinterpret_cast<const typename Pack<T, N>::any *>(row + n - N);
+      v = __builtin_bit_cast(vec, (bits)(__builtin_bit_cast(bits, v) >> (i + N - n) * (int)sizeof(T) * 8));
+    } else {
+      for (int e = 0; e < N; ++e)
+        if (i + e < n) v[e] = row[i + e];
+    }
+  }
   return v;
 }
 
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// As unsigned integers, magnitudes are ordered like their values, infinity behind the finite ones and NaN behind infinity
-__device__ __forceinline__ unsigned wave_max_u(unsigned v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { const unsigned w = __shfl_xor(v, o, 64); v = v > w ? v : w; }
-  return v;
+// As unsigned integers, magnitudes are ordered like their values, infinity behind the finite ones and NaN behind infinity.
+// Maximum and sum over a wave, in every lane: within 16 lanes by moves of the vector unit (quads' neighbours, halves mirrored), then by exchanges of 16 and 32 lanes
+template <int MOVE> __device__ __forceinline__ unsigned moved(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, MOVE, 0xF, 0xF, false); }
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+__device__ __forceinline__ unsigned wave_top(unsigned v) {
+  v = larger(v, moved<0xB1>(v));
+  v = larger(v, moved<0x4E>(v));
+  v = larger(v, moved<0x141>(v));
+  v = larger(v, moved<0x140>(v));
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = larger(r[0], r[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return larger(q[0], q[1]);
+}
+__device__ __forceinline__ float wave_total(float v) {
+  v += __uint_as_float(moved<0xB1>(__float_as_uint(v)));
+  v += __uint_as_float(moved<0x4E>(__float_as_uint(v)));
+  v += __uint_as_float(moved<0x141>(__float_as_uint(v)));
+  v += __uint_as_float(moved<0x140>(__float_as_uint(v)));
+  return sum_xor32(sum_xor16(v));
 }
 
-// Maximum (and sum) over a workgroup of T threads
-template <int T> __device__ __forceinline__ void block_reduce(unsigned &top, float &sum) {
-  __shared__ unsigned tops[T / 64];
-  __shared__ float sums[T / 64];
-  top = wave_max_u(top);
-  sum = wave_sum(sum);
+// Maximum and sum over the T threads of a row (64: of a workgroup's several rows, a wave each)
+template <int T, bool SUM> __device__ __forceinline__ void row_reduce(unsigned &top, float &sum) {
+  top = wave_top(top);
+  if constexpr (SUM) sum = wave_total(sum);
   if constexpr (T > 64) {
-    if ((threadIdx.x & 63) == 0) { tops[threadIdx.x >> 6] = top; sums[threadIdx.x >> 6] = sum; }
+    __shared__ unsigned tops[T / 64];
+    __shared__ float sums[T / 64];
+    if ((threadIdx.x & 63) == 0) { tops[threadIdx.x >> 6] = top; if constexpr (SUM) sums[threadIdx.x >> 6] = sum; }
     __syncthreads();
-    top = tops[0]; sum = sums[0];
+    top = tops[0];
+    if constexpr (SUM) sum = sums[0];
 #pragma unroll
-    for (int w = 1; w < T / 64; ++w) { top = top > tops[w] ? top : tops[w]; sum += sums[w]; }
+    for (int w = 1; w < T / 64; ++w) { top = larger(top, tops[w]); if constexpr (SUM) sum += sums[w]; }
   }
 }
+static constexpr int kWaveRows = 4;                          // rows of a workgroup whose rows are a wave's each
+template <int T> static constexpr int kGroup = T == 64 ? 64 * kWaveRows : T;
 
 // From a value to its code.  ok: the row has codes at all (finite, not tiny).
 // 16-bit rows: x * 127 / max in fp32, corrected by its remainder (all of them times 2^-7, so that nothing overflows), is the correctly rounded quotient; 127 x has at most
@@ -68,11 +97,13 @@ __device__ __forceinline__ unsigned pack_codes(unsigned a, unsigned b, unsigned 
 
 // ---- rows of numbers to codes.  A workgroup of T threads per row; NV > 0: up to NV * 16 bytes a thread stay in registers, NV == 0: the row is read twice.
 template <typename T, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void quantize_q8_kernel(const T *__restrict__ X, int64_t x_stride, int cols, int width, int8_t *__restrict__ codes, int64_t stride,
-                                                              float *__restrict__ scales) {
+__global__ __launch_bounds__(kGroup<THREADS>) void quantize_q8_kernel(const T *__restrict__ X, int64_t x_stride, int rows, int cols, int width, int8_t *__restrict__ codes,
+                                                                      int64_t stride, float *__restrict__ scales) {
   constexpr int N = 16 / sizeof(T);
   typedef typename Pack<T, N>::vec vec;
-  const int64_t row = blockIdx.x;
+  const int64_t row = THREADS == 64 ? (int64_t)blockIdx.x * kWaveRows + (threadIdx.x >> 6) : blockIdx.x;
+  if (THREADS == 64 && row >= rows) return;
+  const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
   const T *x = X + row * x_stride;
   int8_t *out = codes + row * stride;
   unsigned top = 0;
@@ -84,16 +115,16 @@ __global__ __launch_bounds__(THREADS) void quantize_q8_kernel(const T *__restric
   };
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) keep[k] = load_row<T, N>(x, (threadIdx.x + k * THREADS) * N, cols);
+    for (int k = 0; k < NV; ++k) keep[k] = load_row<T, N>(x, (tid + k * THREADS) * N, cols);
 #pragma unroll
     for (int k = 0; k < NV; ++k) look(keep[k]);
   } else {
-    for (int i = threadIdx.x * N; i < cols; i += THREADS * N) look(load_row<T, N>(x, i, cols));
+    for (int i = tid * N; i < cols; i += THREADS * N) look(load_row<T, N>(x, i, cols));
   }
-  block_reduce<THREADS>(top, unused);
+  row_reduce<THREADS, false>(top, unused);
   const float t = __uint_as_float(top);
   const bool finite = top < 0x7f800000u, ok = finite && t >= kTiny;
-  if (threadIdx.x == 0) scales[row] = !finite ? __builtin_nanf("") : ok ? t / 127.0f : 0.f;
+  if (tid == 0) scales[row] = !finite ? __builtin_nanf("") : ok ? t / 127.0f : 0.f;
   const Coder<(sizeof(T) == 2)> code(ok ? t : 1.0f);
   auto emit = [&](int i, const vec &v) {
     if (i >= width) return;
@@ -106,9 +137,9 @@ __global__ __launch_bounds__(THREADS) void quantize_q8_kernel(const T *__restric
   };
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) emit((threadIdx.x + k * THREADS) * N, keep[k]);
+    for (int k = 0; k < NV; ++k) emit((tid + k * THREADS) * N, keep[k]);
   } else {
-    for (int i = threadIdx.x * N; i < width; i += THREADS * N) emit(i, load_row<T, N>(x, i, cols));
+    for (int i = tid * N; i < width; i += THREADS * N) emit(i, load_row<T, N>(x, i, cols));
   }
 }
 
@@ -119,14 +150,16 @@ struct NormArgs {
   int64_t x_stride, add_stride, stride;
   int8_t *codes;
   float *scales;
-  int cols, width;
+  int rows, cols, width;
   float eps;
 };
 struct NoAdd {};
 template <typename TD, typename TG, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS) void rmsnorm_q8_kernel(NormArgs a) {
+__global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a) {
   constexpr bool kAdd = !__is_same(TD, NoAdd);
-  const int64_t row = blockIdx.x;
+  const int64_t row = THREADS == 64 ? (int64_t)blockIdx.x * kWaveRows + (threadIdx.x >> 6) : blockIdx.x;
+  if (THREADS == 64 && row >= a.rows) return;
+  const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
   float *x = a.X + row * a.x_stride;
   const TG *gain = reinterpret_cast<const TG *>(a.gain);
   int8_t *out = a.codes + row * a.stride;
@@ -161,20 +194,20 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_q8_kernel(NormArgs a) {
     typename Pack<TG, 4>::vec g[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int i = (threadIdx.x + k * THREADS) * 4;
+      const int i = (tid + k * THREADS) * 4;
       keep[k] = load_row<float, 4>(x, i, a.cols);
       d[k] = load_add(i);
       g[k] = load_row<TG, 4>(gain, i, a.cols);
     }
 #pragma unroll
-    for (int k = 0; k < NV; ++k) keep[k] = step((threadIdx.x + k * THREADS) * 4, keep[k], d[k], g[k]);
+    for (int k = 0; k < NV; ++k) keep[k] = step((tid + k * THREADS) * 4, keep[k], d[k], g[k]);
   } else {
-    for (int i = threadIdx.x * 4; i < a.cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, a.cols), load_add(i), load_row<TG, 4>(gain, i, a.cols));
+    for (int i = tid * 4; i < a.cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, a.cols), load_add(i), load_row<TG, 4>(gain, i, a.cols));
   }
-  block_reduce<THREADS>(top, ss);
+  row_reduce<THREADS, true>(top, ss);
   const float t = __uint_as_float(top);
   const bool finite = top < 0x7f800000u && ss < __builtin_inff(), ok = finite && t >= kTiny;
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     const float r = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
     a.scales[row] = !finite ? __builtin_nanf("") : ok ? t * r / 127.0f : 0.f;
   }
@@ -184,10 +217,10 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_q8_kernel(NormArgs a) {
   };
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) emit((threadIdx.x + k * THREADS) * 4, keep[k]);
+    for (int k = 0; k < NV; ++k) emit((tid + k * THREADS) * 4, keep[k]);
   } else {
     // each thread reads back what it stored itself
-    for (int i = threadIdx.x * 4; i < a.width; i += THREADS * 4) {
+    for (int i = tid * 4; i < a.width; i += THREADS * 4) {
       f32x4 v = load_row<float, 4>(x, i, a.cols);
       const auto g = load_row<TG, 4>(gain, i, a.cols);
 #pragma unroll
@@ -197,7 +230,8 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_q8_kernel(NormArgs a) {
   }
 }
 
-// ---- back to numbers: code * scale, rounded once more to 16 bits.  256 threads take 8 codes each, of 256 / lanes rows
+// ---- back to numbers: code * scale, rounded once more to 16 bits.  256 threads take 8 codes each, of 256 / lanes rows; where these are too few workgroups for the
+// chip, each of several takes a part of the columns (7 x 12288 MEASURED)
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_q8_kernel(const int8_t *__restrict__ codes, int64_t stride, const float *__restrict__ scales, int rows, int cols, int lanes,
                                                             T *__restrict__ out, int64_t out_stride) {
@@ -206,7 +240,7 @@ __global__ __launch_bounds__(256) void dequantize_q8_kernel(const int8_t *__rest
   const float s = scales[row];
   const int8_t *in = codes + row * stride;
   T *o = out + row * out_stride;
-  for (int i = (threadIdx.x % lanes) * 8; i < cols; i += lanes * 8) {
+  for (int i = (blockIdx.y * lanes + threadIdx.x % lanes) * 8; i < cols; i += gridDim.y * lanes * 8) {
     const uint2 c = *reinterpret_cast<const uint2 *>(in + i);
     f32x4 x[2];
 #pragma unroll
@@ -230,26 +264,46 @@ int check_q8(const prism_q8 *q, const char *who) {
   return PRISM_OK;
 }
 
+// Threads of a row, from its 16-byte pieces and the number of rows.  Few rows are a chain of latencies, so a thread takes one piece, of long rows two or four; many rows fill the
+// chip anyway, and a row of few pieces in many threads is mostly the meeting of its waves.  us at 64, 128, 256, 512, 1024 threads: norm of 24 x 4096 11.1, 4.3, 3.5, 3.2, 3.2; 1 x
+// 12288 24.6, 13.4, 8.2, 4.6, 4.3; 16000 x 500 22.0, 22.7, 27.3, 42.9, 74.3; 16000 x 1003 39.8, 37.3, 40.0, 56.0, 94.4; 16000 x 4096 155, 126, 122, 122, 121; codes of bf16 24 x 12288
+// 13.8, 7.4, 3.7, 3.3, 3.3; 60000 x 1003 35.3, 46.7, 59.3, 94.0, 167; 4099 x 12288 38.4, 45.6, 27.2, 27.1, 26.4.
+static int row_threads(int pieces, int rows) {
+  if (rows < 1024) return pieces <= 64 ? 64 : pieces <= 128 ? 128 : pieces <= 256 ? 256 : pieces <= 1024 ? 512 : 1024;
+  return pieces <= 128 ? 64 : pieces <= 256 ? 128 : pieces <= 1024 ? 256 : pieces <= 2048 ? 512 : 1024;
+}
+// Calls run(threads, pieces of a thread that stay in registers, 0: the row is read twice), both as types, and the grid
+template <typename F> static void for_rows(int pieces, int rows, F &&run) {
+  const int threads = row_threads(pieces, rows), per = (pieces + threads - 1) / threads;
+  auto with = [&](auto t) {
+    constexpr int T = decltype(t)::value;
+    const int grid = T == 64 ? cdiv(rows, kWaveRows) : rows;
+    if constexpr (T < 1024)
+      if (per <= 1) return run(t, std::integral_constant<int, 1>{}, grid);
+    if (per <= 2) return run(t, std::integral_constant<int, 2>{}, grid);
+    if constexpr (T >= 256)
+      if (per <= 4) return run(t, std::integral_constant<int, 4>{}, grid);
+    if constexpr (T == 1024) run(t, std::integral_constant<int, 0>{}, grid);
+  };
+  if (threads == 64) with(std::integral_constant<int, 64>{});
+  else if (threads == 128) with(std::integral_constant<int, 128>{});
+  else if (threads == 256) with(std::integral_constant<int, 256>{});
+  else if (threads == 512) with(std::integral_constant<int, 512>{});
+  else with(std::integral_constant<int, 1024>{});
+}
+
 template <typename T> static void launch_quantize(const void *X, int64_t x_stride, const prism_q8 &q, hipStream_t s) {
-  constexpr int N = 16 / sizeof(T);
-  const int width = q8_width(q.cols), per = (width + 256 * N - 1) / (256 * N);
-  auto run = [&](auto kern, int threads) { kern<<<q.rows, threads, 0, s>>>((const T *)X, x_stride, q.cols, width, q.codes, q.stride, q.scales); };
-  if (width <= 64 * N) run(quantize_q8_kernel<T, 64, 1>, 64);
-  else if (per <= 1) run(quantize_q8_kernel<T, 256, 1>, 256);
-  else if (per <= 2) run(quantize_q8_kernel<T, 256, 2>, 256);
-  else if (per <= 4) run(quantize_q8_kernel<T, 256, 4>, 256);
-  else if (per <= 8) run(quantize_q8_kernel<T, 256, 8>, 256);
-  else run(quantize_q8_kernel<T, 256, 0>, 256);
+  const int width = q8_width(q.cols);
+  for_rows(width / (16 / (int)sizeof(T)), q.rows, [&](auto t, auto nv, int grid) {
+    quantize_q8_kernel<T, decltype(t)::value, decltype(nv)::value>
+        <<<grid, kGroup<decltype(t)::value>, 0, s>>>((const T *)X, x_stride, q.rows, q.cols, width, q.codes, q.stride, q.scales);
+  });
 }
 
 template <typename TD, typename TG> static void launch_norm(const NormArgs &a, int rows, hipStream_t s) {
-  const int per = (a.width + 1023) / 1024;
-  if (a.width <= 256) rmsnorm_q8_kernel<TD, TG, 64, 1><<<rows, 64, 0, s>>>(a);
-  else if (per <= 1) rmsnorm_q8_kernel<TD, TG, 256, 1><<<rows, 256, 0, s>>>(a);
-  else if (per <= 2) rmsnorm_q8_kernel<TD, TG, 256, 2><<<rows, 256, 0, s>>>(a);
-  else if (per <= 4) rmsnorm_q8_kernel<TD, TG, 256, 4><<<rows, 256, 0, s>>>(a);
-  else if (per <= 8) rmsnorm_q8_kernel<TD, TG, 256, 8><<<rows, 256, 0, s>>>(a);
-  else rmsnorm_q8_kernel<TD, TG, 256, 0><<<rows, 256, 0, s>>>(a);
+  for_rows(a.width / 4, rows, [&](auto t, auto nv, int grid) {
+    rmsnorm_q8_kernel<TD, TG, decltype(t)::value, decltype(nv)::value><<<grid, kGroup<decltype(t)::value>, 0, s>>>(a);
+  });
 }
 template <typename TD> static void launch_norm_gain(int gain_dtype, const NormArgs &a, int rows, hipStream_t s) {
   if (gain_dtype == PRISM_DTYPE_FP32) launch_norm<TD, float>(a, rows, s);
@@ -285,7 +339,8 @@ extern "C" int prism_op_dequantize_q8(const prism_q8 *q, int32_t dtype, void *ou
   PRISM_REQUIRE(out && (uintptr_t)out % dtype_size(dtype) == 0, PRISM_EINVAL, "dequantize_q8: output missing or not aligned to its values");
   int lanes = 8;
   while (lanes < 256 && lanes * 8 < q->cols) lanes *= 2;
-  const int grid = cdiv(q->rows, 256 / lanes);
+  const int groups = cdiv(q->rows, 256 / lanes);
+  const dim3 grid(groups, groups < 1024 ? cdiv(q->cols, lanes * 8) : 1);
   auto run = [&](auto *o) { dequantize_q8_kernel<<<grid, 256, 0, (hipStream_t)stream>>>(q->codes, q->stride, q->scales, q->rows, q->cols, lanes, o, out_stride); };
   if (dtype == PRISM_DTYPE_FP32) run((float *)out);
   else if (dtype == PRISM_DTYPE_BF16) run((bf16 *)out);
@@ -304,7 +359,7 @@ extern "C" int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype
   if (out->rows == 0) return PRISM_OK;
   PRISM_REQUIRE(X && gain && (uintptr_t)X % 4 == 0 && (uintptr_t)gain % dtype_size(gain_dtype) == 0 && (!add || (uintptr_t)add % dtype_size(add_dtype) == 0), PRISM_EINVAL,
                 "rmsnorm_q8: X or gain missing, or one not aligned to its values");
-  const NormArgs a{X, add, gain, x_stride, add_stride, out->stride, out->codes, out->scales, out->cols, q8_width(out->cols), eps};
+  const NormArgs a{X, add, gain, x_stride, add_stride, out->stride, out->codes, out->scales, out->rows, out->cols, q8_width(out->cols), eps};
   hipStream_t s = (hipStream_t)stream;
   if (!add) launch_norm_gain<NoAdd>(gain_dtype, a, out->rows, s);
   else if (add_dtype == PRISM_DTYPE_FP32) launch_norm_gain<float>(gain_dtype, a, out->rows, s);
