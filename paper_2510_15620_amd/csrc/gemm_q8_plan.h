@@ -9,10 +9,10 @@ namespace prism {
 
 // A launch deals its tiles over 256 compute units; n = tiles per unit, rounded up.  A tile's time is its slices of 128 codes plus a fixed part (first
 // slice, epilogue), and a slice's time depends on how many tiles share the unit: alone it is a chain of latencies, together the matrix pipes, LDS and
-// the path to the caches.  The constants are fit to 11 tiles and rings on 270 launches of 17 to 20000 rows, N 64-24576, K 64-12288, all epilogues, weights from memory; they
-// are off by 12-18 % (root mean square) where the tile is near the best one, and the pick is on average 1.3 % above the best, 33 % at worst (777 x 2501 x 1003 residual, 15.1 us
-// for 11.4; then 18814 x 256 x 141 residual 13.9 for 11.3, 1154 x 4096 x 12288 residual 103 for 86).
-// Large tiles of fewer rows than 256 take a slice in less time, but not in proportion (256, 192, 160 rows: 1.15, 0.98, 0.91 us); they pay where
+// the path to the caches.  The constants are fit to 11 tiles and rings on 256 launches of 17 to 20000 rows, N 64-24576, K 64-12288, all epilogues, weights from memory; the
+// pick is on average 1.1 % above the best tile, 18 % at worst (3151 x 2712 x 128 residual 21.8 us for 18.4; then 2683 x 14939 x 152 residual 98 for 86, 1202 x 1482 x 376 SwiGLU 6.4
+// for 5.6, 18814 x 256 x 141 residual 13.7 for 11.9, 1543 x 2501 x 1003 stored 12.6 for 11.1).
+// Large tiles of fewer rows than 256 take a slice in less time, but not in proportion (256, 192, 160 rows: 1.13, 0.96, 0.88 us); they pay where
 // their number fills the units better: SwiGLU 391 x 19456 x 2560 42.1 (128 x 64), 39.5 (256), 35.0 (160); 777 x 24576 x 4096 102 (128 x 128), 97 (256), 82 (160); residual 3000 x 4096 x 4096
 // 57.4 (256), 54.5 (192).  Two 128 x 128 tiles a unit lead where K is short: one's epilogue runs beside the other's loop (10782 x 2048 x 432 SwiGLU 26.4, on 256 x 256 32.5).
 struct Q8Tile {
@@ -22,11 +22,11 @@ struct Q8Tile {
 };
 enum { kQ8T256, kQ8T192, kQ8T160, kQ8T128, kQ8T128Deep, kQ8T128x64, kQ8T128x64Deep, kQ8T64, kQ8T32x64, kQ8T64x32, kQ8T32, kQ8Tiles };
 static constexpr Q8Tile kQ8Tile[kQ8Tiles] = {
-    {256, 256, 1, 1.146f, 1.146f, 12.3f, 23.3f, 12.7f}, {192, 256, 1, 0.982f, 0.982f, 9.37f, 18.2f, 9.90f}, {160, 256, 1, 0.914f, 0.914f, 7.27f, 15.7f, 8.57f},
-    {128, 128, 2, 0.662f, 0.469f, 4.05f, 9.43f, 4.63f}, {128, 128, 1, 0.420f, 0.420f, 4.11f, 6.64f, 5.08f},
-    {128, 64, 2, 0.307f, 0.327f, 2.66f, 4.60f, 3.17f}, {128, 64, 1, 0.304f, 0.304f, 2.98f, 4.10f, 3.64f},
-    {64, 64, 2, 0.210f, 0.221f, 2.08f, 2.85f, 2.70f}, {32, 64, 4, 0.223f, 0.179f, 2.47f, 3.12f, 3.23f},
-    {64, 32, 1, 0.140f, 0.140f, 1.96f, 2.21f, 0.f}, {32, 32, 2, 0.089f, 0.108f, 1.72f, 1.91f, 0.f}};
+    {256, 256, 1, 1.128f, 1.128f, 11.6f, 22.4f, 9.63f}, {192, 256, 1, 0.958f, 0.958f, 8.68f, 17.6f, 7.61f}, {160, 256, 1, 0.884f, 0.884f, 6.98f, 15.7f, 6.79f},
+    {128, 128, 2, 0.661f, 0.455f, 3.82f, 9.49f, 3.75f}, {128, 128, 1, 0.437f, 0.437f, 3.95f, 6.56f, 4.41f},
+    {128, 64, 2, 0.312f, 0.319f, 2.57f, 4.63f, 2.93f}, {128, 64, 1, 0.297f, 0.297f, 2.94f, 3.98f, 3.37f},
+    {64, 64, 2, 0.207f, 0.217f, 2.06f, 2.78f, 2.57f}, {32, 64, 4, 0.218f, 0.176f, 2.41f, 3.10f, 2.88f},
+    {64, 32, 1, 0.155f, 0.155f, 1.92f, 2.19f, 0.f}, {32, 32, 2, 0.096f, 0.107f, 1.76f, 1.85f, 0.f}};
 static constexpr double kQ8Launch = 1.3;   // us
 
 enum Q8Epilogue { kQ8Store, kQ8Residual, kQ8Swiglu };
