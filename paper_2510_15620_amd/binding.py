@@ -540,9 +540,17 @@ def op_attention_paged(plan: PagePlan, Q, cache: KVCache, table, out, workspace,
 
 # ---- 8-bit rows ---------------------------------------------------------------------------------------------------------
 
-# Set with the first rows, by which every call gets here: a step of a few tokens waits for the host, so that these calls look nothing up twice
-_DTYPES = {}                # torch dtype -> PRISM_DTYPE_*
-_device = _raw_stream = None
+# Set with the first rows, by which every call gets here: a step of a few tokens waits for the host, so these calls look nothing up twice.
+# torch dtype -> PRISM_DTYPE_*; the current stream of a device; the current device, where there are several
+_DTYPES = {}
+_raw_stream = None
+
+
+def _only_device():
+    return 0
+
+
+_device = _only_device
 
 
 class Q8:
@@ -561,7 +569,9 @@ class Q8:
         if not _DTYPES:
             import torch
             lib()
-            _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+            _raw_stream = torch._C._cuda_getCurrentRawStream
+            if torch.cuda.device_count() > 1:
+                _device = torch._C._cuda_getDevice
             _DTYPES.update({torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16})
         self.codes, self.scales, self.rows, self.cols, self.shape = codes, scales, codes.shape[0], cols, (codes.shape[0], cols)
         self.device = codes.get_device()

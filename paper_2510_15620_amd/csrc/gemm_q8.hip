@@ -14,9 +14,11 @@ namespace prism {
 template <typename OT, int EPI>
 static int launch_kind(int kind, const int8_t *A, const int8_t *W, void *out, int M, int N, int K, hipStream_t s, const Q8Operands &q) {
   switch (kind) {
-    case kQ8T256: return launch_tile<OT, 256, 256, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q);
-    case kQ8T192: return launch_tile<OT, 192, 256, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q);
-    case kQ8T160: return launch_tile<OT, 160, 256, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q);
+    case kQ8T256: return launch_tile<OT, 256, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
+    case kQ8T224: return launch_tile<OT, 224, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
+    case kQ8T192: return launch_tile<OT, 192, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
+    case kQ8T160: return launch_tile<OT, 160, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q);
+    case kQ8T128x256: return launch_tile<OT, 128, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q);
     case kQ8T128: return launch_tile<OT, 128, 128, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q);
     case kQ8T128Deep: return launch_tile<OT, 128, 128, 2, 2, EPI, 5>(A, W, out, M, N, K, s, q);
     case kQ8T128x64: return launch_tile<OT, 128, 64, 4, 1, EPI, 3>(A, W, out, M, N, K, s, q);

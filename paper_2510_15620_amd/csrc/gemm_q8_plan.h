@@ -9,24 +9,26 @@ namespace prism {
 
 // A launch deals its tiles over 256 compute units; n = tiles per unit, rounded up.  A tile's time is its slices of 128 codes plus a fixed part (first
 // slice, epilogue), and a slice's time depends on how many tiles share the unit: alone it is a chain of latencies, together the matrix pipes, LDS and
-// the path to the caches.  The constants are fit to 11 tiles and rings on 256 launches of 17 to 20000 rows, N 64-24576, K 64-12288, all epilogues, weights from memory; the
-// pick is on average 1.1 % above the best tile, 18 % at worst (3151 x 2712 x 128 residual 21.8 us for 18.4; then 2683 x 14939 x 152 residual 98 for 86, 1202 x 1482 x 376 SwiGLU 6.4
-// for 5.6, 18814 x 256 x 141 residual 13.7 for 11.9, 1543 x 2501 x 1003 stored 12.6 for 11.1).
-// Large tiles of fewer rows than 256 take a slice in less time, but not in proportion (256, 192, 160 rows: 1.13, 0.96, 0.88 us); they pay where
-// their number fills the units better: SwiGLU 391 x 19456 x 2560 42.1 (128 x 64), 39.5 (256), 35.0 (160); 777 x 24576 x 4096 102 (128 x 128), 97 (256), 82 (160); residual 3000 x 4096 x 4096
-// 57.4 (256), 54.5 (192).  Two 128 x 128 tiles a unit lead where K is short: one's epilogue runs beside the other's loop (10782 x 2048 x 432 SwiGLU 26.4, on 256 x 256 32.5).
+// the path to the caches.  The constants are fit to 13 tiles and rings on 256 launches of 17 to 20000 rows, N 64-24576, K 64-12288, all epilogues, weights from memory; the
+// pick is on average 0.9 % above the best tile, 22 % at worst (18814 x 256 x 141 residual 13.8 us for 11.3; then 3151 x 2712 x 128 residual 21.9 for 18.7, 18775 x 1037 x 96 residual 46.7
+// for 40.2, 2683 x 14939 x 152 residual 98 for 85, 1543 x 2501 x 1003 stored 12.9 for 11.2).
+// Large tiles of fewer rows than 256 take a slice in less time, but not in proportion; they pay where their number fills the units better, us on 256, 224, 192, 160, 128 rows by 256 columns and
+// on 128 x 128: SwiGLU 600 x 24576 x 4096 91, 85, 77, 70, 67, 71; 1154 x 19456 x 2560 69, 65, 80, 78, 75, 77; 391 x 19456 x 2560 35, 34, 30, 31, 46, 44; stored 1543 x 4096 x 12288 111, 98, 87, 86, 80, 89;
+// 3699 x 2560 x 9728 95, 86, 81, 76, 112, 122; 11520 x 4096 x 12288 394, 443, 409, 433, 451, 498.  Two 128 x 128 tiles a unit lead where K is short: one's epilogue runs beside the
+// other's loop (10782 x 2048 x 432 SwiGLU 26.4, on 256 x 256 32.5).
 struct Q8Tile {
   int bm, bn, occ;                      // tile, workgroups that share a compute unit
   float alone, shared;                  // us per slice: one workgroup on the unit; per workgroup when occ of them share it
   float store, residual, swiglu;        // us per tile
 };
-enum { kQ8T256, kQ8T192, kQ8T160, kQ8T128, kQ8T128Deep, kQ8T128x64, kQ8T128x64Deep, kQ8T64, kQ8T32x64, kQ8T64x32, kQ8T32, kQ8Tiles };
+enum { kQ8T256, kQ8T224, kQ8T192, kQ8T160, kQ8T128x256, kQ8T128, kQ8T128Deep, kQ8T128x64, kQ8T128x64Deep, kQ8T64, kQ8T32x64, kQ8T64x32, kQ8T32, kQ8Tiles };
 static constexpr Q8Tile kQ8Tile[kQ8Tiles] = {
-    {256, 256, 1, 1.128f, 1.128f, 11.6f, 22.4f, 9.63f}, {192, 256, 1, 0.958f, 0.958f, 8.68f, 17.6f, 7.61f}, {160, 256, 1, 0.884f, 0.884f, 6.98f, 15.7f, 6.79f},
-    {128, 128, 2, 0.661f, 0.455f, 3.82f, 9.49f, 3.75f}, {128, 128, 1, 0.437f, 0.437f, 3.95f, 6.56f, 4.41f},
-    {128, 64, 2, 0.312f, 0.319f, 2.57f, 4.63f, 2.93f}, {128, 64, 1, 0.297f, 0.297f, 2.94f, 3.98f, 3.37f},
-    {64, 64, 2, 0.207f, 0.217f, 2.06f, 2.78f, 2.57f}, {32, 64, 4, 0.218f, 0.176f, 2.41f, 3.10f, 2.88f},
-    {64, 32, 1, 0.155f, 0.155f, 1.92f, 2.19f, 0.f}, {32, 32, 2, 0.096f, 0.107f, 1.76f, 1.85f, 0.f}};
+    {256, 256, 1, 1.112f, 1.112f, 11.7f, 22.5f, 9.80f}, {224, 256, 1, 1.009f, 1.009f, 10.6f, 19.9f, 9.18f}, {192, 256, 1, 0.884f, 0.884f, 9.34f, 17.2f, 8.32f},
+    {160, 256, 1, 0.818f, 0.818f, 7.74f, 15.2f, 7.48f}, {128, 256, 1, 0.724f, 0.724f, 6.43f, 12.2f, 6.30f},
+    {128, 128, 2, 0.661f, 0.462f, 3.83f, 9.26f, 3.80f}, {128, 128, 1, 0.456f, 0.456f, 4.05f, 6.56f, 4.46f},
+    {128, 64, 2, 0.307f, 0.325f, 2.55f, 4.58f, 2.91f}, {128, 64, 1, 0.301f, 0.301f, 2.94f, 4.01f, 3.38f},
+    {64, 64, 2, 0.212f, 0.219f, 2.05f, 2.78f, 2.55f}, {32, 64, 4, 0.223f, 0.179f, 2.38f, 3.00f, 2.86f},
+    {64, 32, 1, 0.160f, 0.160f, 1.91f, 2.16f, 0.f}, {32, 32, 2, 0.064f, 0.107f, 1.74f, 1.89f, 0.f}};
 static constexpr double kQ8Launch = 1.3;   // us
 
 enum Q8Epilogue { kQ8Store, kQ8Residual, kQ8Swiglu };
@@ -54,7 +56,7 @@ struct Q8Plan { int rows_first, first, kind; };
 inline Q8Plan q8_plan(int M, int cols, int slices, Q8Epilogue epi) {
   double least;
   Q8Plan p{0, 0, q8_best_tile(M, cols, slices, epi, &least)};
-  for (int k = kQ8T256; k <= kQ8T160; ++k) {
+  for (int k = kQ8T256; k <= kQ8T128x256; ++k) {
     const Q8Tile &t = kQ8Tile[k];
     const int64_t bn = epi == kQ8Swiglu ? t.bn / 2 : t.bn, nN = (cols + bn - 1) / bn, nM = (M + t.bm - 1) / t.bm;
     const int64_t rows = nM * nN / 256 * 256 / nN * t.bm;               // those that fill whole rounds

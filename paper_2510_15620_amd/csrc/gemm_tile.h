@@ -48,8 +48,10 @@ __device__ __forceinline__ int swz(int row, int chunk) { return chunk ^ ((row >>
 // an ulp more and returns 0 where 1 + e^-g exceeds 2^126, values that bf16 still holds.
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
 
-// LDS bytes of a tile's operand stages
-template <int BM, int BN, int S> constexpr int stage_bytes() { return ((BN == 256 ? 3 : S) * BM + S * BN) * BK * 2; }
+// Stages of a tile's operands in LDS, and their bytes.  Tiles of 256 columns: S = 2 is three of A and two of W, 3 two and three, 4 three of both
+template <int BN, int S> constexpr int a_stages() { return BN == 256 ? (S == 3 ? 2 : 3) : S; }
+template <int BN, int S> constexpr int w_stages() { return BN == 256 ? (S == 2 ? 2 : 3) : S; }
+template <int BM, int BN, int S> constexpr int stage_bytes() { return (a_stages<BN, S>() * BM + w_stages<BN, S>() * BN) * BK * 2; }
 
 // OT: type of 16-bit operands and outputs; IT: the operands' (OT or int8_t)
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT = OT>
@@ -69,9 +71,8 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   static_assert(TM * TN * 4 <= 256, "accumulator registers");
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr bool kBig = BN == 256;
-  static_assert(!kBig || S == 2, "the loops of 256 columns have three stages of A and two of W");
-  unsigned char *lA = smem;                                          // [S, or 3 if BN == 256][BM][BK] of two bytes
-  unsigned char *lB = lA + (kBig ? 3 : S) * BM * BK * 2;        // [S][BN][BK]
+  unsigned char *lA = smem;                                          // [stages of A][BM][BK] of two bytes
+  unsigned char *lB = lA + a_stages<BN, S>() * BM * BK * 2;       // [stages of W][BN][BK]
 
   // ---- tile mapping: XCD-contiguous ranges, grouped walk ----
   const int n_tiles = nM * nN;
@@ -514,6 +515,7 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
 #define PRISM_ACC8 PRISM_ACC4, "={a[64:79]}"(acc[4]), "={a[80:95]}"(acc[5]), "={a[96:111]}"(acc[6]), "={a[112:127]}"(acc[7])
 #define PRISM_ACC10 PRISM_ACC8, "={a[128:143]}"(acc[8]), "={a[144:159]}"(acc[9])
 #define PRISM_ACC12 PRISM_ACC10, "={a[160:175]}"(acc[10]), "={a[176:191]}"(acc[11])
+#define PRISM_ACC14 PRISM_ACC12, "={a[192:207]}"(acc[12]), "={a[208:223]}"(acc[13])
 #define PRISM_ACC16                                                                                                               \
   PRISM_ACC4, "={a[64:79]}"(acc[4]), "={a[80:95]}"(acc[5]), "={a[96:111]}"(acc[6]), "={a[112:127]}"(acc[7]),                        \
       "={a[128:143]}"(acc[8]), "={a[144:159]}"(acc[9]), "={a[160:175]}"(acc[10]), "={a[176:191]}"(acc[11]), "={a[192:207]}"(acc[12]), \
@@ -538,8 +540,10 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
     else PRISM_RUN_16(NAME, __VA_ARGS__);                                                                                       \
   } while (0)
   if constexpr (BM == 256) PRISM_RUN(256, PRISM_ACC16);
+  else if constexpr (kBig && BM == 224) PRISM_RUN_Q8(224, 256, PRISM_ACC14);
   else if constexpr (kBig && BM == 192) PRISM_RUN_Q8(192, 256, PRISM_ACC12);
-  else if constexpr (kBig) PRISM_RUN_Q8(160, 256, PRISM_ACC10);
+  else if constexpr (kBig && BM == 160) PRISM_RUN_Q8(160, 256, PRISM_ACC10);
+  else if constexpr (kBig) PRISM_RUN_Q8(128, 256, PRISM_ACC8);
   else if constexpr (kHeads && BM == 64 && S == 6) PRISM_RUN_16(64x128_6_HEAD, PRISM_ACC2);
   else if constexpr (kHeads && BM == 64) PRISM_RUN_16(64x128_3_HEAD, PRISM_ACC2);
   else if constexpr (kHeads && S == 5) PRISM_RUN_16(128x128_5_HEAD, PRISM_ACC4);

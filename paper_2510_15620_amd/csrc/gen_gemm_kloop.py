@@ -6,7 +6,7 @@
 
 A loop sees bytes: slices of 128 bytes a row, fragments of 16 bytes a lane.  The loops on 8-bit integers differ from those on 16-bit values in
 the matrix instruction, 16x16x64 for 16x16x32 from the same registers in the same cycles, in that they may begin anywhere in K and go round (rotated,
-below), integers being exact in any order, and in the large tiles of fewer rows.  Elsewhere in this file k counts 16-bit values.
+below), integers being exact in any order, and in the large tiles' rows and stages (BIG).  Elsewhere in this file k counts 16-bit values.
 
 The 256x256x64 tile.  4 wavefronts (one per SIMD, so each owns 512 registers), wave grid 2x2, wave tile 128x128 = 8x8
 accumulator tiles of v_mfma_f32_16x16x32 kept in 256 AGPRs: the largest wave tile the register file allows, i.e. the
@@ -44,18 +44,23 @@ PREFIX, CLOBBERS = ("PRISM_KLOOP_Q8", "PRISM_KLOOP_Q8_CLOBBERS") if Q8 else ("PR
 MFMA = "v_mfma_i32_16x16x64_i8" if Q8 else 'v_mfma_f32_16x16x32_" TY "'
 
 # ---- register plan (all clobbered) ----
+AB3, AB4 = [112, 113], [114, 115]                                   # as AB and AB2, B stage 2 (8-bit loops)
 AA, AA2, AB, AB2 = [116, 117], [118, 119], [120, 121], [122, 123]   # LDS address of the lane's first fragment row, per step: A stages
                                                                     # 0 and 1, A stage 2, B columns 0-63, B columns 64-127 of the wave
 F = [{"A": [128 + 64 * s + 4 * i for i in range(8)], "B": [160 + 64 * s + 4 * j for j in range(8)]} for s in range(2)]
-CLOBBER_V = list(range(116, 124)) + list(range(128, 256))
-CLOBBER_S = list(range(20, 30))
+CLOBBER_V = list(range(112 if Q8 else 116, 124)) + list(range(128, 256))
+CLOBBER_S = list(range(20, 32 if Q8 else 30))
 
 STAGE = 32768                           # bytes per LDS stage of one operand
-A_STAGES, B_STAGES, PERIOD = 3, 2, 6
 TILE_ROWS = 2048                        # 16 rows x 128 B
-# 256 columns by 32 TM rows: accumulator tiles of a wave by rows, RSTRIDE, PB, LSTRIDE
-BIG = {256: (8, 3, 56, 6), 192: (6, 3, 42, 6), 160: (5, 2, 34, 5)}
-TM, RSTRIDE, PB, LSTRIDE = BIG[256]
+# 256 columns by 32 TM rows: accumulator tiles of a wave by rows, stages of A and of B, RSTRIDE, PB, LSTRIDE.
+# 8-bit launches have three stages of B, weights from memory, and for them two of A up from 192 rows, what LDS holds: A comes out of the caches, where other
+# tiles of its rows have brought it.  us, three of A and two of B -> this: stored 1543 x 4096 x 12288 100 -> 86 (160 rows) and 102 -> 86 (192), 3699 x 2560 x 9728 84 -> 74 (160), SwiGLU
+# 777 x 24576 x 4096 75.7 -> 69.9 (160), many rows 11584 x 24576 x 4096 874 -> 862 (256).
+BIG = {"256": (8, 3, 2, 3, 56, 6)}
+if Q8:
+    BIG = {"256": (8, 2, 3, 3, 56, 6), "224": (7, 2, 3, 3, 49, 6), "192": (6, 2, 3, 3, 42, 6), "160": (5, 3, 3, 2, 34, 5), "128": (4, 3, 3, 2, 27, 4)}
+TM, A_STAGES, B_STAGES, RSTRIDE, PB, LSTRIDE = BIG["256"]
 
 
 def v4(r):
@@ -72,7 +77,9 @@ def reads(fs, k, t):
     sa, sb = t % A_STAGES, t % B_STAGES
     base, off = (AA2, 0) if sa == 2 else (AA, sa * TM * 4096)          # a read's immediate offset ends at 64 KiB
     ra = lambda i: f"ds_read_b128 {v4(F[fs]['A'][i])}, v{base[k]} offset:{off + i * TILE_ROWS}"
-    rb = lambda j: f"ds_read_b128 {v4(F[fs]['B'][j])}, v{(AB if j < 4 else AB2)[k]} offset:{sb * STAGE + j % 4 * TILE_ROWS}"
+    cols = (AB if j < 4 else AB2 for j in range(8)) if sb < 2 else (AB3 if j < 4 else AB4 for j in range(8))
+    cols, sb = list(cols), sb % 2
+    rb = lambda j: f"ds_read_b128 {v4(F[fs]['B'][j])}, v{cols[j][k]} offset:{sb * STAGE + j % 4 * TILE_ROWS}"
     return [ra(0), rb(0), ra(1)] + [rb(j) for j in range(1, 8)] + [ra(i) for i in range(2, TM)]
 
 
@@ -122,6 +129,17 @@ def mfma_order():
     return out
 
 
+def load_order():
+    """The operands (name, stages, loads of a slice) in the order in which a slice asks for them: the one with fewer stages first."""
+    a, b = ("A", A_STAGES, TM), ("B", B_STAGES, 8)
+    return (a, b) if B_STAGES > A_STAGES else (b, a)
+
+
+def flying():
+    """Loads that need not have landed at a slice's barrier: of operands with three stages those of the slice after the next."""
+    return sum(n for _, stages, n in load_order() if stages == 3)
+
+
 def slice_body(t):
     step, whole, n = 8 * TM, 16 * TM, TM + 8            # MFMAs of a step and of the slice; fragment reads of a step, loads of the slice
     behind = {}                                         # position -> what is issued behind that MFMA
@@ -133,10 +151,11 @@ def slice_body(t):
     # stages that were freed by its barrier; the first turn repeats the youngest there, so the first of them sets M0 itself)
     at = [PB + 1 + i * LSTRIDE for i in range(n)]
     tail = next((i for i in range(n) if at[i] >= whole), n)
-    assert tail >= 8
-    for p, l in zip(at[:tail], loads("B", t % B_STAGES) + loads("A", t % A_STAGES)):
+    (w1, s1, n1), (w2, s2, _) = load_order()
+    assert tail >= n1
+    for p, l in zip(at[:tail], loads(w1, t % s1) + loads(w2, t % s2)):
         behind.setdefault(p, []).append(l)
-    for p, l in zip(at[tail:], loads("A", (t - 1) % A_STAGES, tail - 8)[tail - 8:]):
+    for p, l in zip(at[tail:], loads(w2, (t - 1) % s2, tail - n1)[tail - n1:]):
         behind.setdefault(p - whole, []).append(l)
     assert (n - 1) * RSTRIDE < PB < step and at[-1] - whole < PB
     out = []
@@ -144,7 +163,7 @@ def slice_body(t):
         if m in (0, step):
             out.append("s_waitcnt lgkmcnt(0)")          # the step's fragments; of 256 rows the last was requested 18 MFMAs ago
         if m == PB:
-            out += [f"s_waitcnt vmcnt({TM}) lgkmcnt(0)"] + advance("A") + advance("B") + ["s_barrier"]
+            out += [f"s_waitcnt vmcnt({flying()}) lgkmcnt(0)"] + advance("A") + advance("B") + ["s_barrier"]
         out.append(mfma(m // step, *mfma_order()[m % step]))
         out += behind.get(m, [])
     return out
@@ -155,16 +174,21 @@ def kloop():
     for k in range(2):                                  # the steps' addresses differ only in a swizzled chunk bit
         s += [f"v_xor_b32 v{r[k]}, {64 * k}, %[{a}]" for r, a in ((AA, "aa"), (AB, "ab"), (AB2, "ab2"))]
         s += [f"v_add_u32 v{AA2[k]}, {2 * TM * 4096}, v{AA[k]}"]
+        s += [f"v_add_u32 v{r3[k]}, {2 * STAGE}, v{r[k]}" for r3, r in ((AB3, AB), (AB4, AB2))] if B_STAGES == 3 else []
     s += ["s_mov_b64 s[20:21], %[pa]", "s_mov_b64 s[22:23], %[pb]", "s_mov_b32 s24, %[nk]", "s_sub_u32 s26, %[nk], 1",
           "s_mov_b32 s25, 0", "s_mov_b32 s29, 0"] + (["s_sub_u32 s31, %[wr], 1"] if Q8 else [])
-    # ---- prologue: B and A of slices 0 and 1, A of slice 2; the accumulators are cleared while the first of them arrive
-    s += loads("B", 0) + advance("B") + loads("A", 0) + advance("A") + loads("B", 1) + loads("A", 1) + advance("A") + loads("A", 2)
+    # ---- prologue: both operands of slices 0 and 1, those with three stages of slice 2; the accumulators are cleared while the first of them arrive
+    for t in range(3):
+        for which, stages, _ in load_order():
+            if t < stages:
+                s += loads(which, t) + (advance(which) if t + 1 < stages else [])
     s += [f"v_accvgpr_write_b32 a{r}, 0" for r in range(32 * TM)]
-    s += [f"s_waitcnt vmcnt({8 + 2 * TM})", "s_barrier"] + reads(0, 0, 0)
+    s += [f"s_waitcnt vmcnt({8 + TM + flying()})", "s_barrier"] + reads(0, 0, 0)
     s += ["L_loop_%=:"]
-    for t in range(PERIOD):
+    period = math.lcm(A_STAGES, B_STAGES)
+    for t in range(period):
         s += slice_body(t) + ["s_sub_u32 s24, s24, 1", "s_cmp_eq_u32 s24, 0"]
-        s += ["s_cbranch_scc1 L_done_%="] if t + 1 < PERIOD else ["s_cbranch_scc0 L_loop_%="]
+        s += ["s_cbranch_scc1 L_done_%="] if t + 1 < period else ["s_cbranch_scc0 L_loop_%="]
     s += ["L_done_%=:", "s_waitcnt vmcnt(0) lgkmcnt(0)", "s_nop 15", "s_nop 15"]   # MFMA results settle before the epilogue reads them
     return s
 
@@ -333,7 +357,7 @@ def emit(name, lines):
 
 
 def main():
-    global TM, RSTRIDE, PB, LSTRIDE
+    global TM, A_STAGES, B_STAGES, RSTRIDE, PB, LSTRIDE
     print("// Generated by gen_gemm_kloop.py - do not edit.  See that file for the schedule.")
     if Q8:
         print("// PRISM_KLOOP_Q8_<tile>: as PRISM_KLOOP_<tile>, sums of 8-bit integers; bk = 128 - a row's bytes, wr slices from where pa / pb point to the row's end.")
@@ -343,10 +367,10 @@ def main():
         print("// (step 0, stage 0); ga / gb byte offset from pa / pb of the chunk this lane fetches in each of its wave's load instructions,")
         print("// less 1024 (j % 4); la / lb LDS byte address of the first row the first of them fills (stage 0, uniform); nk number of slices.")
     print()
-    for rows in BIG if Q8 else [256]:
-        TM, RSTRIDE, PB, LSTRIDE = BIG[rows]
-        emit(f"{PREFIX}_{rows}" + ("" if Q8 else "(TY)"), kloop())
-    regs = ", ".join(f'"v{r}"' for r in CLOBBER_V) + ", " + ", ".join(f'"s{r}"' for r in CLOBBER_S + ([30, 31] if Q8 else []))
+    for name in BIG:
+        TM, A_STAGES, B_STAGES, RSTRIDE, PB, LSTRIDE = BIG[name]
+        emit(f"{PREFIX}_{name}" + ("" if Q8 else "(TY)"), kloop())
+    regs = ", ".join(f'"v{r}"' for r in CLOBBER_V) + ", " + ", ".join(f'"s{r}"' for r in CLOBBER_S)
     for c in SMALL:
         if not (Q8 and (c.name.endswith("HEAD") or c.name == "128x128_4")):
             c.emit()
