@@ -11,7 +11,7 @@ namespace prism {
 // slice, epilogue), and a slice's time depends on how many tiles share the unit: alone it is a chain of latencies, together the matrix pipes, LDS and
 // the path to the caches.  The constants are fit to 13 tiles and rings on 256 launches of 17 to 20000 rows, N 64-24576, K 64-12288, all epilogues, weights from memory; the
 // pick is on average 0.9 % above the best tile, 22 % at worst (18814 x 256 x 141 residual 13.8 us for 11.3; then 3151 x 2712 x 128 residual 21.9 for 18.7, 18775 x 1037 x 96 residual 46.7
-// for 40.2, 2683 x 14939 x 152 residual 98 for 85, 1543 x 2501 x 1003 stored 12.9 for 11.2).
+// for 40.2, 2683 x 14939 x 152 residual 98 for 85).
 // Large tiles of fewer rows than 256 take a slice in less time, but not in proportion; they pay where their number fills the units better, us on 256, 224, 192, 160, 128 rows by 256 columns and
 // on 128 x 128: SwiGLU 600 x 24576 x 4096 91, 85, 77, 70, 67, 71; 1154 x 19456 x 2560 69, 65, 80, 78, 75, 77; 391 x 19456 x 2560 35, 34, 30, 31, 46, 44; stored 1543 x 4096 x 12288 111, 98, 87, 86, 80, 89;
 // 3699 x 2560 x 9728 95, 86, 81, 76, 112, 122; 11520 x 4096 x 12288 394, 443, 409, 433, 451, 498.  Two 128 x 128 tiles a unit lead where K is short: one's epilogue runs beside the
@@ -35,9 +35,11 @@ enum Q8Epilogue { kQ8Store, kQ8Residual, kQ8Swiglu };
 
 inline double q8_tile_time(const Q8Tile &t, int64_t M, int64_t cols, int slices, Q8Epilogue epi) {
   const int bn = epi == kQ8Swiglu ? t.bn / 2 : t.bn;
-  const int64_t n = ((M + t.bm - 1) / t.bm * ((cols + bn - 1) / bn) + 255) / 256, full = n / t.occ, rest = n % t.occ;
-  const double slice = full * std::max<double>(t.alone, t.shared * t.occ) + (rest ? std::max<double>(t.alone, t.shared * rest) : 0.);
-  return kQ8Launch + slices * slice + (double)(full + (rest > 0)) * (epi == kQ8Swiglu ? t.swiglu : epi == kQ8Residual ? t.residual : t.store);
+  const int64_t tiles = (M + t.bm - 1) / t.bm * ((cols + bn - 1) / bn), n = (tiles + 255) / 256, rounds = (n + t.occ - 1) / t.occ, last = n - (rounds - 1) * t.occ;
+  // the last of `last` tiles that share a unit shares the caches with few, where it is on few units: 260 tiles of 128 x 128 (1543 x 2501 x 1003) 11.2 us
+  const double fill = std::min(1., 0.7 + (double)(tiles - (n - 1) * 256) / 256), sharing = last > 1 ? (double)(last - 1) + fill : 1.;
+  const double slice = (double)(rounds - 1) * std::max<double>(t.alone, t.shared * t.occ) + std::max<double>(t.alone, t.shared * sharing);
+  return kQ8Launch + slices * slice + (double)rounds * (epi == kQ8Swiglu ? t.swiglu : epi == kQ8Residual ? t.residual : t.store);
 }
 inline int q8_best_tile(int64_t M, int64_t cols, int slices, Q8Epilogue epi, double *time) {
   int at = 0;
