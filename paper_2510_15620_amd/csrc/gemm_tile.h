@@ -566,18 +566,23 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   epilogue();
 }
 
+static constexpr int kDevices = 64;      // of a process
+
 // One launch of a tile over M rows.  K: units of two bytes that the loop reads.
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT, typename Extra>
 static int launch_tile(const IT *A, const IT *W, void *out, int M, int N, int K, hipStream_t s, const Extra &extra) {
   constexpr size_t lds = stage_bytes<BM, BN, S>();
   auto kern = gemm_16_kernel<OT, BM, BN, WM, WN, EPI, S, IT>;
-  // the attribute is per function: set once per process, also when several contexts launch from different threads
-  static std::once_flag attr_once;
-  static hipError_t attr_rc = hipSuccess;
-  std::call_once(attr_once, [&] {
-    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  // the attribute is per function and device: set once for each, also when several contexts launch from different threads
+  static std::once_flag attr_once[kDevices];
+  static hipError_t attr_rc[kDevices];
+  int device = 0;
+  PRISM_HIP(hipGetDevice(&device));
+  PRISM_REQUIRE(device < kDevices, PRISM_EUNSUPPORTED, "gemm: device %d", device);
+  std::call_once(attr_once[device], [&] {
+    attr_rc[device] = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   });
-  PRISM_HIP(attr_rc);
+  PRISM_HIP(attr_rc[device]);
   const int ncols = EPI == PRISM_EPI_SWIGLU ? N / 2 : N, bn_out = EPI == PRISM_EPI_SWIGLU ? BN / 2 : BN;
   const int nM = cdiv(M, BM), nN = cdiv(ncols, bn_out);
   const int grid = cdiv((int64_t)nM * nN, 8) * 8;
