@@ -3,9 +3,11 @@
 //
 // The sum is exact: |a w| <= 2^14 and K < 2^17, so it fits 32-bit integers.  It is converted to fp32 (2^-24), multiplied by sa and then by sw (2^-24 each).
 // v_mfma_i32_16x16x64_i8 takes twice the k of the 16-bit instruction from the same bytes in the same cycles, so the kernel is
-// the 16-bit products' (gemm_tile.h): a row of K codes is read as K / 2 16-bit values, and a product takes the time of a 16-bit one of half its K, at the same clock
-// (11520 x 4096 x 12288: 480 us, in half with K = 6144 479, both at 1.6 GHz, where the chip's power is spent).  Codes behind a row's end are zeros up to
-// a multiple of 128, a slice of the loop, so the loop has no tail.
+// the 16-bit products' (gemm_tile.h): a row of K codes is read as K / 2 16-bit values, and in one loop a product takes the time of a 16-bit one of half its K, at the same
+// clock (11520 x 4096 x 12288 with residual 480 us, in half with K = 6144 479, both at 1.6 GHz).  What 8 bits change is what a loop half as long shows: the epilogue (gemm_q8.h)
+// and how soon weights have to arrive (gen_gemm_kloop.py: BIG; the same product then 411).  11584 x 24576 x 4096 with SwiGLU: 807 to 847 us, 2.75 to 2.89 POP/s, by the chip; of that
+// 17 rounds of tiles, matrix pipes busy 70 % of the cycles, a tile's epilogue some 11000 cycles of 90000.
+// Codes behind a row's end are zeros up to a multiple of 128, a slice of the loop, so the loop has no tail.
 #include "gemm_tile.h"
 #include "gemm_q8_plan.h"
 
