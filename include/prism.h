@@ -412,7 +412,7 @@ int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype, const voi
 /* Y[m,n] = A.scales[m] W.scales[n] sum_k A[m,k] W[n,k] with the epilogues of prism_op_gemm: STORE and SWIGLU to BF16 or F16 (half saturates, NaN stays NaN),
  * STORE_F32 and RESIDUAL to FP32; out has A->rows rows of W->rows values (SWIGLU: half as many), out_stride values apart (up to 2^23).  The sum of
  * integers is exact, everything behind it is fp32.  W's rows together are below 4 GiB - 8 KiB.  out must not overlap the operands.
- * The order of nothing depends on timing: same inputs, same bits. */
+ * A row's bits depend on that row and W alone (as those of the other calls on its own numbers): not on the rows beside it, not on timing. */
 int prism_op_gemm_q8(int32_t epilogue, const prism_q8 *A, const prism_q8 *W, int32_t out_dtype, void *out, int64_t out_stride, void *stream);
 
 /* Intermediate scorer (Sec. 4.1): for each sequence c, the last token's state through the final RMSNorm and

@@ -59,19 +59,32 @@ __device__ __forceinline__ float wave_total(float v) {
   return sum_xor32(sum_xor16(v));
 }
 
-// Maximum and sum over the T threads of a row (64: of a workgroup's several rows, a wave each)
-template <int T, bool SUM> __device__ __forceinline__ void row_reduce(unsigned &top, float &sum) {
+// Maximum over the T threads of a row (64: of a workgroup's several rows, a wave each), and the sum of NS pieces a thread has.  Piece k of thread t is piece t + k T of the row: 64 pieces
+// are summed by a wave, and these sums one after the other in the row's order, so that a row's bits do not depend on how many threads it has, which goes by the number of rows
+template <int T, int NS> __device__ __forceinline__ void row_reduce(unsigned &top, float (&piece)[NS > 0 ? NS : 1], float &sum) {
   top = wave_top(top);
-  if constexpr (SUM) sum = wave_total(sum);
+#pragma unroll
+  for (int k = 0; k < NS; ++k) piece[k] = wave_total(piece[k]);
   if constexpr (T > 64) {
     __shared__ unsigned tops[T / 64];
-    __shared__ float sums[T / 64];
-    if ((threadIdx.x & 63) == 0) { tops[threadIdx.x >> 6] = top; if constexpr (SUM) sums[threadIdx.x >> 6] = sum; }
+    __shared__ float sums[NS > 0 ? NS * (T / 64) : 1];
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      tops[w] = top;
+#pragma unroll
+      for (int k = 0; k < NS; ++k) sums[k * (T / 64) + w] = piece[k];
+    }
     __syncthreads();
     top = tops[0];
-    if constexpr (SUM) sum = sums[0];
 #pragma unroll
-    for (int w = 1; w < T / 64; ++w) { top = larger(top, tops[w]); if constexpr (SUM) sum += sums[w]; }
+    for (int v = 1; v < T / 64; ++v) top = larger(top, tops[v]);
+    sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < NS * (T / 64); ++v) sum += sums[v];
+  } else {
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) sum += piece[k];
   }
 }
 static constexpr int kWaveRows = 4;                          // rows of a workgroup whose rows are a wave's each
@@ -107,7 +120,7 @@ __global__ __launch_bounds__(kGroup<THREADS>) void quantize_q8_kernel(const T *_
   const T *x = X + row * x_stride;
   int8_t *out = codes + row * stride;
   unsigned top = 0;
-  float unused = 0.f;
+  float none[1], unused;
   vec keep[NV > 0 ? NV : 1];
   auto look = [&](const vec &v) {
 #pragma unroll
@@ -121,7 +134,7 @@ __global__ __launch_bounds__(kGroup<THREADS>) void quantize_q8_kernel(const T *_
   } else {
     for (int i = tid * N; i < cols; i += THREADS * N) look(load_row<T, N>(x, i, cols));
   }
-  row_reduce<THREADS, false>(top, unused);
+  row_reduce<THREADS, 0>(top, none, unused);
   const float t = __uint_as_float(top);
   const bool finite = top < 0x7f800000u, ok = finite && t >= kTiny;
   if (tid == 0) scales[row] = !finite ? __builtin_nanf("") : ok ? t / 127.0f : 0.f;
@@ -164,10 +177,11 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
   const TG *gain = reinterpret_cast<const TG *>(a.gain);
   int8_t *out = a.codes + row * a.stride;
   unsigned top = 0;
-  float ss = 0.f;
-  f32x4 keep[NV > 0 ? NV : 1];
+  constexpr int NS = NV > 0 ? NV : 1;
+  float squares[NS] = {}, ss;
+  f32x4 keep[NS];
   // x gain of four values; x with the addition is stored, its squares are summed
-  auto step = [&](int i, f32x4 v, const auto &d, const typename Pack<TG, 4>::vec &g) {
+  auto step = [&](int i, f32x4 v, const auto &d, const typename Pack<TG, 4>::vec &g, float &squares) {
     if constexpr (kAdd) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += to_f32(d[e]);
@@ -178,7 +192,7 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      ss += v[e] * v[e];
+      squares += v[e] * v[e];
       v[e] *= to_f32(g[e]);
       const unsigned m = magnitude(v[e]);
       top = top > m ? top : m;
@@ -200,11 +214,11 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
       g[k] = load_row<TG, 4>(gain, i, a.cols);
     }
 #pragma unroll
-    for (int k = 0; k < NV; ++k) keep[k] = step((tid + k * THREADS) * 4, keep[k], d[k], g[k]);
+    for (int k = 0; k < NV; ++k) keep[k] = step((tid + k * THREADS) * 4, keep[k], d[k], g[k], squares[k]);
   } else {
-    for (int i = tid * 4; i < a.cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, a.cols), load_add(i), load_row<TG, 4>(gain, i, a.cols));
+    for (int i = tid * 4; i < a.cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, a.cols), load_add(i), load_row<TG, 4>(gain, i, a.cols), squares[0]);
   }
-  row_reduce<THREADS, true>(top, ss);
+  row_reduce<THREADS, NS>(top, squares, ss);
   const float t = __uint_as_float(top);
   const bool finite = top < 0x7f800000u && ss < __builtin_inff(), ok = finite && t >= kTiny;
   if (tid == 0) {

@@ -157,8 +157,8 @@ def test_dequantize(cols, dtype):
 
 def check_norm(x, d, gain, eps, q, got_x):
     """x: what the stream held (fp32, host).  The stream is fl(x + d) to the bit.  p = x gain, its maximum, 127 / max and the product of both are rounded: 4 u of 127 around the
-    half step.  The scale: a sum of squares whose longest chain is 4 values per 1024 of the row (in 256 threads, shorter in other kernels), then 6 + 4 additions and the square itself, halved by the
-    root; the mean's division, eps, root, reciprocal, p, two products, one more in hand: 8."""
+    half step.  The scale: a sum of squares, of which a value meets 4 others of its piece, 6 times the other lanes and a sum for every 256 values of the row (rows of more than 16384: 4 values for every
+    4096, then 16 sums, which is fewer), and the square itself, at most 4 for every 1024 and 11, halved by the root; the mean's division, eps, root, reciprocal, p, two products, one more in hand: 8."""
     want_x = x + d.float() if d is not None else x
     assert torch.equal(got_x, want_x)
     n, cols = want_x.double() * gain.double(), x.shape[1]
@@ -206,6 +206,21 @@ def test_norm_extremes(cols):
     assert torch.equal(torch.isnan(q.scales.cpu()), bad) and not codes_of(q)[bad].any()
     ok = B.Q8.of(q.codes[:, :cols][~bad.cuda()].contiguous(), q.scales[~bad.cuda()].contiguous())
     check_norm(x[~bad], d[~bad], gain, 1e-6, ok, X.cpu()[~bad])
+
+
+@pytest.mark.parametrize("cols", [64, 500, 1003, 2048, 4096, 9000, 12288, 16384, 20003])
+def test_rows_do_not_depend_on_the_rows_beside_them(cols):
+    """One row, a hundred and two thousand take different numbers of threads a row: same bits of stream, codes and scales."""
+    x, d, gain = torch.randn(2000, cols, device="cuda"), torch.randn(2000, cols, device="cuda").to(BF16), torch.randn(cols, device="cuda")
+    X, q, p = x.clone(), B.Q8(2000, cols), B.Q8(2000, cols)
+    B.op_rmsnorm_q8(X, gain, 1e-6, q, add=d)
+    B.op_quantize_q8(d, p)
+    for n in (1, 100):
+        Y, r = x[:n].clone(), B.Q8(n, cols)
+        B.op_rmsnorm_q8(Y, gain, 1e-6, r, add=d[:n])
+        assert torch.equal(Y, X[:n]) and torch.equal(r.codes, q.codes[:n]) and torch.equal(r.scales, q.scales[:n])
+        B.op_quantize_q8(d[:n], r)
+        assert torch.equal(r.codes, p.codes[:n]) and torch.equal(r.scales, p.scales[:n])
 
 
 def test_norm_strides():
@@ -386,6 +401,41 @@ def test_gemm_is_the_same_at_every_size_of_the_batch():
             part[m] = 3.0
             B.op_gemm_q8(epilogue, A.first(m), W, part[:m])
             assert torch.equal(part[:m], full[:m]) and (part[m] == 3).all(), (epilogue, m)
+
+
+@pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
+def test_gemm_of_one_column(epilogue, dtype):
+    for M, N, K in ((1, 1, 3), (8, 3, 1), (65, 1, 130), (300, 5, 1003), (5000, 1, 128), (1, 1, 131071)):
+        run_product(M, N * (2 if epilogue == B.EPI_SWIGLU else 1), K, epilogue, dtype)
+
+
+def test_rows_behind_four_gib():
+    """Rows whose offsets pass 32 bits, in values and in bytes: the last ones give what they give by themselves."""
+    rows, cols, tail = 530000, 8192, 1000
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda")
+    x.view(torch.int16).random_(0x3c00, 0x3f80)                # numbers from 2^-7 up to 1
+    q, part = B.Q8(rows, cols), B.Q8(tail, cols)
+    B.op_quantize_q8(x, q)
+    B.op_quantize_q8(x[-tail:], part)
+    assert torch.equal(q.codes[-tail:], part.codes) and torch.equal(q.scales[-tail:], part.scales)
+    _, _, w, sw = operands(1, 66, cols, 10)
+    W = B.Q8.of(w, sw)
+    out, alone = torch.empty(rows, 66, device="cuda"), torch.empty(tail, 66, device="cuda")
+    B.op_gemm_q8(B.EPI_STORE_F32, q, W, out)
+    B.op_gemm_q8(B.EPI_STORE_F32, part, W, alone)
+    assert torch.equal(out[-tail:], alone)
+    check_product(B.EPI_STORE_F32, F32, alone, None, product(part.codes, part.scales, w, sw))
+    back = torch.empty(rows, cols, dtype=F16, device="cuda")
+    B.op_dequantize_q8(q, back)
+    assert torch.equal(back[-tail:].double(), (part.codes.float() * part.scales[:, None]).half().double())
+    del x, back
+    X = torch.ones(rows, cols, device="cuda")
+    X[-tail:] = torch.randn(tail, cols, generator=gen(11)).cuda()
+    last = X[-tail:].clone()
+    gain = torch.ones(cols, device="cuda")
+    B.op_rmsnorm_q8(X, gain, 1e-6, q, add=torch.full((rows, cols), 0.5, dtype=F16, device="cuda"))
+    B.op_rmsnorm_q8(last, gain, 1e-6, part, add=torch.full_like(last, 0.5))
+    assert torch.equal(X[-tail:], last) and torch.equal(q.codes[-tail:], part.codes) and torch.equal(q.scales[-tail:], part.scales)
 
 
 def test_empty_calls():
