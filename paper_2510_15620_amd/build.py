@@ -21,6 +21,10 @@ COMMON = ["--offload-arch=gfx950", "-O3", *os.environ.get("PRISM_EXTRA_FLAGS", "
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # the pruning decisions must reproduce a fixed fp64 operation order: no fused multiply-add
 EXTRA = {"prune.hip": ["-ffp-contract=off"]}
+# the first arguments of a launch in registers when it starts: small launches' first loads wait for one latency less (products of 8-bit
+# rows, us: 391 x 4096 x 1024 6.84 -> 6.60, 100 x 1024 x 1024 3.85 -> 3.60, 64 x 6144 x 1024 with SwiGLU 5.9 -> 5.7)
+for _f in ("gemm_q8.hip", "gemm_q8_rows.hip", "q8.hip"):
+    EXTRA[_f] = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
 
 
 def _compile(src: str) -> str:

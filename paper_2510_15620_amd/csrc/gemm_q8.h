@@ -5,11 +5,9 @@
 
 namespace prism {
 
-// What a product of 8-bit rows brings: a scale for each row of A and of W, the distance of the rows in bytes (multiples of 16), and
-// the distance of the output's rows in values; of the tiles, by how many slices of K a column tile begins behind the one before it (0: all begin at K's start).
+// What a product of 8-bit rows brings: a scale for each row of A and of W, and the distance of the output's rows in values; of the tiles, by how many slices of K a column tile begins behind the one before it (0: all begin at K's start).
 struct Q8Operands {
   const float *sa, *sw;
-  uint32_t lda, ldw;
   int64_t ldo;
   int turn;
 };

@@ -14,24 +14,24 @@
 namespace prism {
 
 template <typename OT, int EPI>
-static int launch_kind(int kind, const int8_t *A, const int8_t *W, void *out, int M, int N, int K, hipStream_t s, const Q8Operands &q) {
+static int launch_kind(int kind, const int8_t *A, const int8_t *W, void *out, int M, int N, int K, hipStream_t s, const Q8Operands &q, uint32_t lda, uint32_t ldw) {
   switch (kind) {
-    case kQ8T256: return launch_tile<OT, 256, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
-    case kQ8T224: return launch_tile<OT, 224, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
-    case kQ8T192: return launch_tile<OT, 192, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q);
-    case kQ8T160: return launch_tile<OT, 160, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q);
-    case kQ8T128x256: return launch_tile<OT, 128, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q);
-    case kQ8T128: return launch_tile<OT, 128, 128, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q);
-    case kQ8T128Deep: return launch_tile<OT, 128, 128, 2, 2, EPI, 5>(A, W, out, M, N, K, s, q);
-    case kQ8T128x64: return launch_tile<OT, 128, 64, 4, 1, EPI, 3>(A, W, out, M, N, K, s, q);
-    case kQ8T128x64Deep: return launch_tile<OT, 128, 64, 4, 1, EPI, 6>(A, W, out, M, N, K, s, q);
-    case kQ8T64: return launch_tile<OT, 64, 64, 2, 2, EPI, 5>(A, W, out, M, N, K, s, q);
-    case kQ8T32x64: return launch_tile<OT, 32, 64, 1, 1, EPI, 4>(A, W, out, M, N, K, s, q);
+    case kQ8T256: return launch_tile<OT, 256, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T224: return launch_tile<OT, 224, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T192: return launch_tile<OT, 192, 256, 2, 2, EPI, 3>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T160: return launch_tile<OT, 160, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T128x256: return launch_tile<OT, 128, 256, 2, 2, EPI, 4>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T128: return launch_tile<OT, 128, 128, 2, 2, EPI, 2>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T128Deep: return launch_tile<OT, 128, 128, 2, 2, EPI, 5>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T128x64: return launch_tile<OT, 128, 64, 4, 1, EPI, 3>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T128x64Deep: return launch_tile<OT, 128, 64, 4, 1, EPI, 6>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T64: return launch_tile<OT, 64, 64, 2, 2, EPI, 5>(A, W, out, M, N, K, s, q, lda, ldw);
+    case kQ8T32x64: return launch_tile<OT, 32, 64, 1, 1, EPI, 4>(A, W, out, M, N, K, s, q, lda, ldw);
     default: break;
   }
   if constexpr (EPI != PRISM_EPI_SWIGLU) {
-    if (kind == kQ8T64x32) return launch_tile<OT, 64, 32, 2, 1, EPI, 7>(A, W, out, M, N, K, s, q);
-    return launch_tile<OT, 32, 32, 2, 2, EPI, 9>(A, W, out, M, N, K, s, q);
+    if (kind == kQ8T64x32) return launch_tile<OT, 64, 32, 2, 1, EPI, 7>(A, W, out, M, N, K, s, q, lda, ldw);
+    return launch_tile<OT, 32, 32, 2, 2, EPI, 9>(A, W, out, M, N, K, s, q, lda, ldw);
   }
   return PRISM_EUNSUPPORTED;
 }
@@ -43,8 +43,9 @@ static int launch_epi(const prism_q8 &a, const prism_q8 &w, void *out, int64_t o
   const int N = w.rows, slices = q8_width(a.cols) / kQ8Slice;
   const Q8Plan p = q8_plan(a.rows, kGlu ? N / 2 : N, slices, kGlu ? kQ8Swiglu : EPI == PRISM_EPI_RESIDUAL ? kQ8Residual : kQ8Store);
   auto rows_on = [&](int kind, int m0, int rows) {
-    const Q8Operands q{a.scales + m0, w.scales, (uint32_t)a.stride, (uint32_t)w.stride, out_stride, q8_turn(a.rows, w.stride)};
-    return launch_kind<OT, EPI>(kind, a.codes + m0 * a.stride, w.codes, reinterpret_cast<char *>(out) + m0 * out_stride * out_elem, rows, N, slices * BK, s, q);
+    const Q8Operands q{a.scales + m0, w.scales, out_stride, q8_turn(a.rows, w.stride)};
+    return launch_kind<OT, EPI>(kind, a.codes + m0 * a.stride, w.codes, reinterpret_cast<char *>(out) + m0 * out_stride * out_elem, rows, N, slices * BK, s, q, (uint32_t)a.stride,
+                                (uint32_t)w.stride);
   };
   if (p.rows_first > 0) PRISM_TRY(rows_on(p.first, 0, p.rows_first));
   return rows_on(p.kind, p.rows_first, a.rows - p.rows_first);

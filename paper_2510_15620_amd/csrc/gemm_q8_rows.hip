@@ -12,8 +12,8 @@ namespace prism {
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 template <typename OT, int EPI, int MT, int NT, int NW, int D>
-__global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, const int8_t *W, void *out_, int M, int N, int slices, uint32_t bytesA, uint32_t bytesW,
-                                                               Q8Operands q) {
+__global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, const int8_t *W, int M, int N, int slices, uint32_t bytesA, uint32_t bytesW,
+                                                               uint32_t lda, uint32_t ldw, void *out_, Q8Operands q) {
   constexpr bool kGlu = EPI == PRISM_EPI_SWIGLU, kF32 = EPI == PRISM_EPI_RESIDUAL || EPI == PRISM_EPI_STORE_F32;
   constexpr int NO = kGlu ? NT / 2 : NT;                     // tiles of 16 output columns
   constexpr int ITEMS = MT * NO, PER = (ITEMS + NW - 1) / NW; // output tiles; of a wave
@@ -26,11 +26,11 @@ __global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, 
   const auto rA = __builtin_amdgcn_make_buffer_rsrc((void *)A, 0, (int)bytesA, 0x00027000), rW = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)bytesW, 0x00027000);
   uint32_t oA[MT], oW[NT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) { const int m = i * 16 + row; oA[i] = (uint32_t)(m < M ? m : M - 1) * q.lda + group * 16u; }
+  for (int i = 0; i < MT; ++i) { const int m = i * 16 + row; oA[i] = (uint32_t)(m < M ? m : M - 1) * lda + group * 16u; }
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int up = kGlu && j >= NO, c = n0 + (j - up * NO) * 16 + row;
-    oW[j] = (uint32_t)((c < F ? c : F - 1) + up * F) * q.ldw + group * 16u;
+    oW[j] = (uint32_t)((c < F ? c : F - 1) + up * F) * ldw + group * 16u;
   }
   i32x4 a[D][MT][2], w[D][NT][2], acc[MT][NT] = {};
   auto load = [&](int u, int turn) __attribute__((always_inline)) {
@@ -138,9 +138,9 @@ template <typename OT, int EPI, int MT, int NT, int NW, int D>
 static int launch(const prism_q8 &a, const prism_q8 &w, void *out, int64_t out_stride, hipStream_t s) {
   constexpr int NO = EPI == PRISM_EPI_SWIGLU ? NT / 2 : NT;
   const int F = EPI == PRISM_EPI_SWIGLU ? w.rows / 2 : w.rows, width = q8_width(a.cols);
-  const Q8Operands q{a.scales, w.scales, (uint32_t)a.stride, (uint32_t)w.stride, out_stride, 0};
-  gemm_q8_rows_kernel<OT, EPI, MT, NT, NW, D><<<cdiv(F, NO * 16), NW * 64, 0, s>>>(a.codes, w.codes, out, a.rows, w.rows, width / kQ8Slice,
-                                                                                  (uint32_t)((a.rows - 1) * a.stride + width), (uint32_t)((w.rows - 1) * w.stride + width), q);
+  const Q8Operands q{a.scales, w.scales, out_stride, 0};
+  gemm_q8_rows_kernel<OT, EPI, MT, NT, NW, D><<<cdiv(F, NO * 16), NW * 64, 0, s>>>(a.codes, w.codes, a.rows, w.rows, width / kQ8Slice, (uint32_t)((a.rows - 1) * a.stride + width),
+                                                                                  (uint32_t)((w.rows - 1) * w.stride + width), (uint32_t)a.stride, (uint32_t)w.stride, out, q);
   PRISM_HIP(hipGetLastError());
   return PRISM_OK;
 }

@@ -53,10 +53,11 @@ template <int BN, int S> constexpr int a_stages() { return BN == 256 ? (S == 3 ?
 template <int BN, int S> constexpr int w_stages() { return BN == 256 ? (S == 2 ? 2 : 3) : S; }
 template <int BM, int BN, int S> constexpr int stage_bytes() { return (a_stages<BN, S>() * BM + w_stages<BN, S>() * BN) * BK * 2; }
 
+// lda, ldw: bytes from row to row of 8-bit operands (multiples of 16), in front of what the loop does not wait for, so that they arrive in registers with the launch (build.py)
 // OT: type of 16-bit operands and outputs; IT: the operands' (OT or int8_t)
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT = OT>
 __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 : 2)) void gemm_16_kernel(
-    const IT *__restrict__ A, const IT *__restrict__ W, void *__restrict__ out_, int M, int N, int K, int nM, int nN,
+    const IT *__restrict__ A, const IT *__restrict__ W, int M, int N, int K, int nM, int nN, uint32_t lda, uint32_t ldw, void *__restrict__ out_,
     std::conditional_t<std::is_same_v<IT, int8_t>, Q8Operands, QkvEpilogue> qe) {
   constexpr bool kQ8 = std::is_same_v<IT, int8_t>;
   constexpr int NW = WM * WN;
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
   constexpr uint32_t kBias = 4096;
   uint32_t gA[A_ITERS], gB[B_ITERS];
   uint32_t rowA = (uint32_t)K * 2u, rowB = rowA;                     // bytes from row to row
-  if constexpr (kQ8) { rowA = qe.lda; rowB = qe.ldw; }
+  if constexpr (kQ8) { rowA = lda; rowB = ldw; }
 #pragma unroll
   for (int j = 0; j < A_ITERS; ++j) {
     const int row = (wave * A_ITERS + j) * 8 + lrow;
@@ -568,9 +569,9 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
 
 static constexpr int kDevices = 64;      // of a process
 
-// One launch of a tile over M rows.  K: units of two bytes that the loop reads.
+// One launch of a tile over M rows.  K: units of two bytes that the loop reads; lda, ldw: of 8-bit operands
 template <typename OT, int BM, int BN, int WM, int WN, int EPI, int S, typename IT, typename Extra>
-static int launch_tile(const IT *A, const IT *W, void *out, int M, int N, int K, hipStream_t s, const Extra &extra) {
+static int launch_tile(const IT *A, const IT *W, void *out, int M, int N, int K, hipStream_t s, const Extra &extra, uint32_t lda = 0, uint32_t ldw = 0) {
   constexpr size_t lds = stage_bytes<BM, BN, S>();
   auto kern = gemm_16_kernel<OT, BM, BN, WM, WN, EPI, S, IT>;
   // the attribute is per function and device: set once for each, also when several contexts launch from different threads
@@ -586,7 +587,7 @@ static int launch_tile(const IT *A, const IT *W, void *out, int M, int N, int K,
   const int ncols = EPI == PRISM_EPI_SWIGLU ? N / 2 : N, bn_out = EPI == PRISM_EPI_SWIGLU ? BN / 2 : BN;
   const int nM = cdiv(M, BM), nN = cdiv(ncols, bn_out);
   const int grid = cdiv((int64_t)nM * nN, 8) * 8;
-  kern<<<grid, WM * WN * 64, lds, s>>>(A, W, out, M, N, K, nM, nN, extra);
+  kern<<<grid, WM * WN * 64, lds, s>>>(A, W, M, N, K, nM, nN, lda, ldw, out, extra);
   PRISM_HIP(hipGetLastError());
   return PRISM_OK;
 }

@@ -160,22 +160,23 @@ __global__ __launch_bounds__(kGroup<THREADS>) void quantize_q8_kernel(const T *_
 struct NormArgs {
   float *X;
   const void *add, *gain;
-  int64_t x_stride, add_stride, stride;
-  int8_t *codes;
-  float *scales;
-  int rows, cols, width;
+  int x_stride, add_stride, rows, cols, width;
   float eps;
+  int8_t *codes;
+  int64_t stride;
+  float *scales;
 };
 struct NoAdd {};
 template <typename TD, typename TG, int THREADS, int NV>
-__global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a) {
+__global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(float *X, const void *add, const void *gain_, int x_stride, int add_stride, int rows, int cols,
+                                                                     int width, float eps, int8_t *codes, int64_t stride, float *scales) {
   constexpr bool kAdd = !__is_same(TD, NoAdd);
   const int64_t row = THREADS == 64 ? (int64_t)blockIdx.x * kWaveRows + (threadIdx.x >> 6) : blockIdx.x;
-  if (THREADS == 64 && row >= a.rows) return;
+  if (THREADS == 64 && row >= rows) return;
   const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-  float *x = a.X + row * a.x_stride;
-  const TG *gain = reinterpret_cast<const TG *>(a.gain);
-  int8_t *out = a.codes + row * a.stride;
+  float *x = X + row * x_stride;
+  const TG *gain = reinterpret_cast<const TG *>(gain_);
+  int8_t *out = codes + row * stride;
   unsigned top = 0;
   constexpr int NS = NV > 0 ? NV : 1;
   float squares[NS] = {}, ss;
@@ -185,10 +186,10 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
     if constexpr (kAdd) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += to_f32(d[e]);
-      if (i + 4 <= a.cols) *reinterpret_cast<typename Pack<float, 4>::any *>(x + i) = v;
+      if (i + 4 <= cols) *reinterpret_cast<typename Pack<float, 4>::any *>(x + i) = v;
       else
         for (int e = 0; e < 4; ++e)
-          if (i + e < a.cols) x[i + e] = v[e];
+          if (i + e < cols) x[i + e] = v[e];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
     return v;
   };
   auto load_add = [&](int i) {
-    if constexpr (kAdd) return load_row<TD, 4>(reinterpret_cast<const TD *>(a.add) + row * a.add_stride, i, a.cols);
+    if constexpr (kAdd) return load_row<TD, 4>(reinterpret_cast<const TD *>(add) + row * add_stride, i, cols);
     else return 0;
   };
   if constexpr (NV > 0) {
@@ -209,34 +210,34 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(NormArgs a)
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int i = (tid + k * THREADS) * 4;
-      keep[k] = load_row<float, 4>(x, i, a.cols);
+      keep[k] = load_row<float, 4>(x, i, cols);
       d[k] = load_add(i);
-      g[k] = load_row<TG, 4>(gain, i, a.cols);
+      g[k] = load_row<TG, 4>(gain, i, cols);
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) keep[k] = step((tid + k * THREADS) * 4, keep[k], d[k], g[k], squares[k]);
   } else {
-    for (int i = tid * 4; i < a.cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, a.cols), load_add(i), load_row<TG, 4>(gain, i, a.cols), squares[0]);
+    for (int i = tid * 4; i < cols; i += THREADS * 4) step(i, load_row<float, 4>(x, i, cols), load_add(i), load_row<TG, 4>(gain, i, cols), squares[0]);
   }
   row_reduce<THREADS, NS>(top, squares, ss);
   const float t = __uint_as_float(top);
   const bool finite = top < 0x7f800000u && ss < __builtin_inff(), ok = finite && t >= kTiny;
   if (tid == 0) {
-    const float r = 1.0f / sqrtf(ss / (float)a.cols + a.eps);
-    a.scales[row] = !finite ? __builtin_nanf("") : ok ? t * r / 127.0f : 0.f;
+    const float r = 1.0f / sqrtf(ss / (float)cols + eps);
+    scales[row] = !finite ? __builtin_nanf("") : ok ? t * r / 127.0f : 0.f;
   }
   const Coder<false> code(ok ? t : 1.0f);
   auto emit = [&](int i, const f32x4 &v) {
-    if (i < a.width) *reinterpret_cast<unsigned *>(out + i) = ok ? pack_codes(code(v[0]), code(v[1]), code(v[2]), code(v[3])) : 0u;
+    if (i < width) *reinterpret_cast<unsigned *>(out + i) = ok ? pack_codes(code(v[0]), code(v[1]), code(v[2]), code(v[3])) : 0u;
   };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) emit((tid + k * THREADS) * 4, keep[k]);
   } else {
     // each thread reads back what it stored itself
-    for (int i = tid * 4; i < a.width; i += THREADS * 4) {
-      f32x4 v = load_row<float, 4>(x, i, a.cols);
-      const auto g = load_row<TG, 4>(gain, i, a.cols);
+    for (int i = tid * 4; i < width; i += THREADS * 4) {
+      f32x4 v = load_row<float, 4>(x, i, cols);
+      const auto g = load_row<TG, 4>(gain, i, cols);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= to_f32(g[e]);
       emit(i, v);
@@ -316,7 +317,8 @@ template <typename T> static void launch_quantize(const void *X, int64_t x_strid
 
 template <typename TD, typename TG> static void launch_norm(const NormArgs &a, int rows, hipStream_t s) {
   for_rows(a.width / 4, rows, [&](auto t, auto nv, int grid) {
-    rmsnorm_q8_kernel<TD, TG, decltype(t)::value, decltype(nv)::value><<<grid, kGroup<decltype(t)::value>, 0, s>>>(a);
+    rmsnorm_q8_kernel<TD, TG, decltype(t)::value, decltype(nv)::value><<<grid, kGroup<decltype(t)::value>, 0, s>>>(
+        a.X, a.add, a.gain, a.x_stride, a.add_stride, a.rows, a.cols, a.width, a.eps, a.codes, a.stride, a.scales);
   });
 }
 template <typename TD> static void launch_norm_gain(int gain_dtype, const NormArgs &a, int rows, hipStream_t s) {
@@ -373,7 +375,7 @@ extern "C" int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype
   if (out->rows == 0) return PRISM_OK;
   PRISM_REQUIRE(X && gain && (uintptr_t)X % 4 == 0 && (uintptr_t)gain % dtype_size(gain_dtype) == 0 && (!add || (uintptr_t)add % dtype_size(add_dtype) == 0), PRISM_EINVAL,
                 "rmsnorm_q8: X or gain missing, or one not aligned to its values");
-  const NormArgs a{X, add, gain, x_stride, add_stride, out->stride, out->codes, out->scales, out->rows, out->cols, q8_width(out->cols), eps};
+  const NormArgs a{X, add, gain, (int)x_stride, (int)add_stride, out->rows, out->cols, q8_width(out->cols), eps, out->codes, out->stride, out->scales};
   hipStream_t s = (hipStream_t)stream;
   if (!add) launch_norm_gain<NoAdd>(gain_dtype, a, out->rows, s);
   else if (add_dtype == PRISM_DTYPE_FP32) launch_norm_gain<float>(gain_dtype, a, out->rows, s);
