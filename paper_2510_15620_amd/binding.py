@@ -585,10 +585,15 @@ class Q8:
         _need(codes.dim() == 2 and codes.dtype is torch.int8 and codes.is_cuda and codes.get_device() == torch.cuda.current_device(),
               "Q8.of: codes [rows, cols] int8 on the current device")
         _need(scales.shape == codes.shape[:1] and scales.dtype is torch.float32 and scales.device == codes.device, "Q8.of: a fp32 scale for each row")
-        q = cls(*codes.shape)
-        q.codes[:, codes.shape[1]:] = 0
-        q.codes[:, :codes.shape[1]] = codes
-        q.scales.copy_(scales)
+        rows, cols = codes.shape
+        _need(cols > 0, f"Q8: {rows} rows of {cols} codes")
+        if cols % 128:
+            padded = codes.new_zeros(rows, (cols + 127) // 128 * 128)
+            padded[:, :cols] = codes
+        else:
+            padded = codes.clone(memory_format=torch.contiguous_format)
+        q = cls.__new__(cls)
+        q._set(padded, scales.clone(memory_format=torch.contiguous_format), cols)
         return q
 
     def first(self, rows: int) -> "Q8":

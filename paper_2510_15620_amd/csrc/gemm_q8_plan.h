@@ -29,24 +29,25 @@ static constexpr Q8Tile kQ8Tile[kQ8Tiles] = {
     {128, 64, 2, 0.307f, 0.325f, 2.55f, 4.58f, 2.91f}, {128, 64, 1, 0.301f, 0.301f, 2.94f, 4.01f, 3.38f},
     {64, 64, 2, 0.212f, 0.219f, 2.05f, 2.78f, 2.55f}, {32, 64, 4, 0.223f, 0.179f, 2.38f, 3.00f, 2.86f},
     {64, 32, 1, 0.160f, 0.160f, 1.91f, 2.16f, 0.f}, {32, 32, 2, 0.064f, 0.107f, 1.74f, 1.89f, 0.f}};
-static constexpr double kQ8Launch = 1.3;   // us
+static constexpr float kQ8Launch = 1.3f;   // us
 
 enum Q8Epilogue { kQ8Store, kQ8Residual, kQ8Swiglu };
 
-inline double q8_tile_time(const Q8Tile &t, int64_t M, int64_t cols, int slices, Q8Epilogue epi) {
-  const int bn = epi == kQ8Swiglu ? t.bn / 2 : t.bn;
-  const int64_t tiles = (M + t.bm - 1) / t.bm * ((cols + bn - 1) / bn), n = (tiles + 255) / 256, rounds = (n + t.occ - 1) / t.occ, last = n - (rounds - 1) * t.occ;
+// (M and cols up to PRISM_MAX_STEP, so that all counts fit 32 bits: their divisions are most of a plan's time on the host, 0.1 us for few rows)
+inline float q8_tile_time(const Q8Tile &t, uint32_t M, uint32_t cols, int slices, Q8Epilogue epi) {
+  const uint32_t bm = (uint32_t)t.bm, bn = (uint32_t)(epi == kQ8Swiglu ? t.bn / 2 : t.bn), occ = (uint32_t)t.occ;
+  const uint32_t tiles = (M + bm - 1) / bm * ((cols + bn - 1) / bn), n = (tiles + 255) / 256, rounds = (n + occ - 1) / occ, last = n - (rounds - 1) * occ;
   // the last of `last` tiles that share a unit shares the caches with few, where it is on few units: 260 tiles of 128 x 128 (1543 x 2501 x 1003) 11.2 us
-  const double fill = std::min(1., 0.7 + (double)(tiles - (n - 1) * 256) / 256), sharing = last > 1 ? (double)(last - 1) + fill : 1.;
-  const double slice = (double)(rounds - 1) * std::max<double>(t.alone, t.shared * t.occ) + std::max<double>(t.alone, t.shared * sharing);
-  return kQ8Launch + slices * slice + (double)rounds * (epi == kQ8Swiglu ? t.swiglu : epi == kQ8Residual ? t.residual : t.store);
+  const float fill = std::min(1.f, 0.7f + (float)(tiles - (n - 1) * 256) / 256.f), sharing = last > 1 ? (float)(last - 1) + fill : 1.f;
+  const float slice = (float)(rounds - 1) * std::max(t.alone, t.shared * (float)occ) + std::max(t.alone, t.shared * sharing);
+  return kQ8Launch + (float)slices * slice + (float)rounds * (epi == kQ8Swiglu ? t.swiglu : epi == kQ8Residual ? t.residual : t.store);
 }
-inline int q8_best_tile(int64_t M, int64_t cols, int slices, Q8Epilogue epi, double *time) {
+inline int q8_best_tile(uint32_t M, uint32_t cols, int slices, Q8Epilogue epi, float *time) {
   int at = 0;
-  *time = 1e30;
+  *time = 1e30f;
   for (int k = 0; k < kQ8Tiles; ++k) {
     if (epi == kQ8Swiglu && kQ8Tile[k].bn == 32) continue;              // SwiGLU pairs a gate and an up tile in a wave
-    const double t = q8_tile_time(kQ8Tile[k], M, cols, slices, epi);
+    const float t = q8_tile_time(kQ8Tile[k], M, cols, slices, epi);
     if (t < *time) { *time = t; at = k; }
   }
   return at;
@@ -56,17 +57,18 @@ inline int q8_best_tile(int64_t M, int64_t cols, int slices, Q8Epilogue epi, dou
 // of large tiles may fill only a few compute units at a whole tile's price.
 struct Q8Plan { int rows_first, first, kind; };
 inline Q8Plan q8_plan(int M, int cols, int slices, Q8Epilogue epi) {
-  double least;
-  Q8Plan p{0, 0, q8_best_tile(M, cols, slices, epi, &least)};
+  float least;
+  Q8Plan p{0, 0, q8_best_tile((uint32_t)M, (uint32_t)cols, slices, epi, &least)};
   for (int k = kQ8T256; k <= kQ8T128x256; ++k) {
     const Q8Tile &t = kQ8Tile[k];
-    const int64_t bn = epi == kQ8Swiglu ? t.bn / 2 : t.bn, nN = (cols + bn - 1) / bn, nM = (M + t.bm - 1) / t.bm;
-    const int64_t rows = nM * nN / 256 * 256 / nN * t.bm;               // those that fill whole rounds
-    if (rows <= 0 || rows >= M) continue;
-    double rest;
-    const int kind = q8_best_tile(M - rows, cols, slices, epi, &rest);
-    const double both = q8_tile_time(t, rows, cols, slices, epi) + rest;
-    if (both < 0.98 * least) { least = both; p = {(int)rows, k, kind}; }
+    const uint32_t bm = (uint32_t)t.bm, bn = (uint32_t)(epi == kQ8Swiglu ? t.bn / 2 : t.bn), nN = ((uint32_t)cols + bn - 1) / bn, nM = ((uint32_t)M + bm - 1) / bm;
+    if (nM * nN <= 256) continue;
+    const uint32_t rows = nM * nN / 256 * 256 / nN * bm;                // those that fill whole rounds
+    if (rows == 0 || rows >= (uint32_t)M) continue;
+    float rest;
+    const int kind = q8_best_tile((uint32_t)M - rows, (uint32_t)cols, slices, epi, &rest);
+    const float both = q8_tile_time(t, rows, (uint32_t)cols, slices, epi) + rest;
+    if (both < 0.98f * least) { least = both; p = {(int)rows, k, kind}; }
   }
   return p;
 }
