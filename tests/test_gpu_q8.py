@@ -503,7 +503,7 @@ def test_a_block(rows, hidden, ffn, dtype):
 
 def test_a_block_captured_and_replayed():
     """One graph, replayed on changing inputs between eager work: every replay gives the eager calls' bits.  Two graphs of the same weights on two streams do not meet."""
-    eager, a, b = (block_buffers(130, 512, 1536, F16, 8) for _ in range(3))
+    eager, a, b = (block_buffers(130, 512, 1408, F16, 8) for _ in range(3))
     for buf in (eager, a, b):
         block(*buf)
     torch.cuda.synchronize()
@@ -528,6 +528,32 @@ def test_a_block_captured_and_replayed():
         torch.cuda.synchronize()
         for buf in (a, b):
             assert torch.equal(buf[8], eager[8]) and torch.equal(buf[0], eager[0]) and torch.equal(buf[7].codes, eager[7].codes), turn
+
+
+def test_blocks_in_two_threads():
+    """Two threads, a stream each, the same weights: nothing is shared but what is read."""
+    import threading
+    want = [block_buffers(60 + 300 * i, 512, 1408, F16, 12 + i) for i in range(2)]
+    got = [block_buffers(60 + 300 * i, 512, 1408, F16, 12 + i) for i in range(2)]
+    shared = got[0][3:5]
+    torch.cuda.synchronize()
+
+    def run(i):
+        buf = got[i][:3] + shared + got[i][5:]
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                block(*buf)
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for i in range(2):
+        buf = want[i][:3] + shared + want[i][5:]
+        for _ in range(20):
+            block(*buf)
+        assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][8], want[i][8]) and torch.equal(got[i][7].codes, want[i][7].codes)
 
 
 def test_weights_in_eight_bits_stand_for_the_weights():
