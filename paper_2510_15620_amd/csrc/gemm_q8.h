@@ -12,6 +12,13 @@ struct Q8Operands {
   int turn;
 };
 
+// A sum times its scales, each product rounded: never one operation with the addition to a stream behind it, which the kernel of few rows has in the same registers
+// and the tiles behind LDS.  A quarter of the stream's values would differ in their last bit between the two, and a row's bits go by the row and W alone.
+__device__ __forceinline__ float q8_scaled(int sum, float sa, float sw) {
+#pragma clang fp contract(off)
+  return (float)sum * sa * sw;
+}
+
 // silu(g) * u of the 8-bit products, off by 6.5 + 1.5 |g| in 2^-24 (exponential, its argument, sum, reciprocal, two products).  Their loops are half as long
 // as the 16-bit ones, so that the epilogue is a quarter of a tile of K = 4096, and a division's ten instructions show (with the two-at-a-time rounding below, us: 11520 x 24576 x 4096
 // 895 -> 847, x 1024 355 -> 313; the rounding alone, stored 11520 x 12288 x 4096 450 -> 432).  Where 1 + e^-g

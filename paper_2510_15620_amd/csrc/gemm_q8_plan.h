@@ -1,4 +1,4 @@
-// Which kernel a product of 8-bit rows runs on, by estimates of time.  The result does not depend on it: the sums are exact.  (No device code:
+// Which kernel a product of 8-bit rows runs on, by estimates of time.  The result does not depend on it: the sums are exact and every kernel rounds what is behind them alike.  (No device code:
 // tests compile this file by itself.)
 #pragma once
 

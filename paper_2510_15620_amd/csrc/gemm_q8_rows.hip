@@ -105,7 +105,7 @@ __global__ __launch_bounds__(NW * 64) void gemm_q8_rows_kernel(const int8_t *A, 
       for (int v = 1; v < NW; ++v) sum += part[v][tile][lane];
       f32x4 y;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = (float)sum[k] * sa[e] * scale[k];
+      for (int k = 0; k < 4; ++k) y[k] = q8_scaled(sum[k], sa[e], scale[k]);
       return y;
     };
     f32x4 y = total(i * NT + j, sw[e][0]);

@@ -242,7 +242,7 @@ __global__ __launch_bounds__(WM *WN * 64, (stage_bytes<BM, BN, S>() > 81920 ? 1 
     if constexpr (kQ8) {
       int n;
       asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(n) : "a"(acc[t / 4][t % 4 * 4 + q]));
-      return (float)n * sa[i] * sw[j][q];
+      return q8_scaled(n, sa[i], sw[j][q]);
     } else {
       float r;
       asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(acc[t / 4][t % 4 * 4 + q]));

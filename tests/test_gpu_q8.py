@@ -404,6 +404,22 @@ def test_gemm_is_the_same_at_every_size_of_the_batch():
 
 
 @pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
+@pytest.mark.parametrize("N,K", [(1030, 777), (512, 4224), (9000, 700), (6000, 1000), (4096, 1024)])
+def test_gemm_of_a_stream_is_the_same_at_every_size_of_the_batch(N, K, epilogue, dtype):
+    """The same over an output that holds numbers: what is added to the stream is rounded before the addition in the kernel of few rows and in all tiles.  The
+    first takes up to 8, 16, 32 or 64 rows here."""
+    a, sa, w, sw = operands(2100, N, K, 6)
+    A, W, cols = B.Q8.of(a, sa), B.Q8.of(w, sw), N // 2 if epilogue == B.EPI_SWIGLU else N
+    old = torch.randn(2100, cols, generator=torch.Generator(device="cuda").manual_seed(N), device="cuda").to(dtype)
+    full = old.clone()
+    B.op_gemm_q8(epilogue, A, W, full)
+    for m in (1, 8, 9, 16, 17, 32, 33, 64, 65, 200, 500, 1100):
+        part = old[:m + 1].clone()
+        B.op_gemm_q8(epilogue, A.first(m), W, part[:m])
+        assert torch.equal(part[:m], full[:m]) and torch.equal(part[m], old[m]), (m, int((part[:m] != full[:m]).sum()))
+
+
+@pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
 def test_gemm_of_one_column(epilogue, dtype):
     for M, N, K in ((1, 1, 3), (8, 3, 1), (65, 1, 130), (300, 5, 1003), (5000, 1, 128), (1, 1, 131071)):
         run_product(M, N * (2 if epilogue == B.EPI_SWIGLU else 1), K, epilogue, dtype)
