@@ -405,7 +405,7 @@ int prism_op_dequantize_q8(const prism_q8 *q, int32_t dtype, void *out, int64_t 
 
 /* Residual addition, RMSNorm and quantisation in one pass: X[t,:] += add[t,:] (fp32, stored; add may be NULL), then the rows of X / sqrt(mean(X^2) + eps) * gain to
  * out (out->rows rows of out->cols).  add and gain [cols] of any dtype each.  The normed values are not rounded before they are quantised.  1e-30 <= eps < 1e30.
- * A row whose squares' sum is beyond fp32 counts as one with an infinity.  add must not overlap X. */
+ * A row whose squares' sum, products with gain or normed values are beyond fp32 counts as one with an infinity.  add must not overlap X. */
 int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype, const void *add, int64_t add_stride, int32_t gain_dtype, const void *gain,
                         float eps, const prism_q8 *out, void *stream);
 

@@ -221,11 +221,12 @@ __global__ __launch_bounds__(kGroup<THREADS>) void rmsnorm_q8_kernel(float *X, c
   }
   row_reduce<THREADS, NS>(top, squares, ss);
   const float t = __uint_as_float(top);
-  const bool finite = top < 0x7f800000u && ss < __builtin_inff(), ok = finite && t >= kTiny;
-  if (tid == 0) {
-    const float r = 1.0f / sqrtf(ss / (float)cols + eps);
-    scales[row] = !finite ? __builtin_nanf("") : ok ? t * r / 127.0f : 0.f;
-  }
+  bool finite = top < 0x7f800000u && ss < __builtin_inff();
+  auto largest = [&] { return t * (1.0f / sqrtf(ss / (float)cols + eps)); };      // of the normed row
+  // (r is 10^15 at most, eps being 10^-30 at least: the normed values of ordinary rows are known to be finite without it)
+  if (t >= 0x1p78f) finite = finite && largest() < __builtin_inff();
+  const bool ok = finite && t >= kTiny;
+  if (tid == 0) scales[row] = !finite ? __builtin_nanf("") : ok ? largest() / 127.0f : 0.f;
   const Coder<false> code(ok ? t : 1.0f);
   auto emit = [&](int i, const f32x4 &v) {
     if (i < width) *reinterpret_cast<unsigned *>(out + i) = ok ? pack_codes(code(v[0]), code(v[1]), code(v[2]), code(v[3])) : 0u;

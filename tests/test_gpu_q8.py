@@ -208,6 +208,29 @@ def test_norm_extremes(cols):
     check_norm(x[~bad], d[~bad], gain, 1e-6, ok, X.cpu()[~bad])
 
 
+@pytest.mark.parametrize("cols", [64, 1003, 4096, 20003])
+def test_norm_of_rows_whose_normed_values_leave_fp32(cols):
+    """A row whose stream and products with the gain are finite, but not its norm, is one with an infinity, as one is whose products with the gain are not; large rows
+    whose norm is finite keep their codes."""
+    x, gain = torch.zeros(4, cols), torch.ones(cols)
+    gain[1], gain[2] = 3e38, 1e38 / cols ** 0.5
+    x[0, 1] = 1.0                                               # normed: 3e38 sqrt(cols)
+    x[1, 2], x[1, 3] = 1.7, 1e-3                                # about 1e38
+    x[2, 1], x[2, 3] = 2.0, 1.0                                 # 6e38 before the division
+    x[3] = 1.0
+    x[3, 1] = 0.0
+    q = B.Q8(4, cols)
+    q.codes.fill_(55)
+    X = x.cuda()
+    B.op_rmsnorm_q8(X, gain.cuda(), 1e-6, q)
+    assert torch.equal(X.cpu(), x)
+    s, c = q.scales.cpu(), codes_of(q)
+    assert torch.isnan(s[[0, 2]]).all() and not c[[0, 2]].any(), (s, c[:, :4])
+    assert torch.isfinite(s[[1, 3]]).all() and c[1, 2] == 127 and c[3, 2] == 127
+    ok = B.Q8.of(q.codes[1::2, :cols].contiguous(), q.scales[1::2].contiguous())
+    check_norm(x[1::2], None, gain, 1e-6, ok, X.cpu()[1::2])
+
+
 @pytest.mark.parametrize("cols", [64, 500, 1003, 2048, 4096, 9000, 12288, 16384, 20003])
 def test_rows_do_not_depend_on_the_rows_beside_them(cols):
     """One row, a hundred and two thousand take different numbers of threads a row: same bits of stream, codes and scales."""
