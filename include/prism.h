@@ -388,8 +388,8 @@ int prism_op_attention_paged(const prism_page_shape *shape, const prism_kv_cache
  *
  * Row r stands for the numbers codes[r * stride + c] * scales[r], c < cols, with scale = max|x| / 127 and code = x / scale rounded to the nearest integer,
  * ties to even.  A row with a NaN or an infinity has a scale of NaN and codes of 0, so that what is computed of it is NaN; a row whose largest magnitude is below
- * 2^-119 has a scale of 0 and codes of 0.  Codes behind cols are 0 up to a multiple of 128 (the makers write them; a caller's own rows have to
- * have them, and may have codes of -128). */
+ * 2^-119 has a scale of 0 and codes of 0 (prism_op_rmsnorm_q8: before the division, see there).  Codes behind cols are 0 up to a multiple of 128 (the makers write
+ * them; a caller's own rows have to have them, and may have codes of -128). */
 typedef struct {
   int8_t *codes;                      /* [device], 16-byte aligned */
   float  *scales;                     /* [device] [rows] */
@@ -405,7 +405,9 @@ int prism_op_dequantize_q8(const prism_q8 *q, int32_t dtype, void *out, int64_t 
 
 /* Residual addition, RMSNorm and quantisation in one pass: X[t,:] += add[t,:] (fp32, stored; add may be NULL), then the rows of X / sqrt(mean(X^2) + eps) * gain to
  * out (out->rows rows of out->cols).  add and gain [cols] of any dtype each.  The normed values are not rounded before they are quantised.  1e-30 <= eps < 1e30.
- * A row whose squares' sum, products with gain or normed values are beyond fp32 counts as one with an infinity.  add must not overlap X. */
+ * The limit of 2^-119 is on |X gain|: a row below it is zeros whatever the division makes of it, and a row above it that a large eps makes small keeps its codes
+ * with a scale that may be subnormal (fewer digits) or 0.  A row whose squares' sum, products with gain or normed values are beyond fp32 counts as one with an
+ * infinity.  add must not overlap X. */
 int prism_op_rmsnorm_q8(float *X, int64_t x_stride, int32_t add_dtype, const void *add, int64_t add_stride, int32_t gain_dtype, const void *gain,
                         float eps, const prism_q8 *out, void *stream);
 

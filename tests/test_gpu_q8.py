@@ -231,6 +231,56 @@ def test_norm_of_rows_whose_normed_values_leave_fp32(cols):
     check_norm(x[1::2], None, gain, 1e-6, ok, X.cpu()[1::2])
 
 
+@pytest.mark.parametrize("eps", [1.5e-30, 1e-6, 0.9e30])
+@pytest.mark.parametrize("cols", [64, 1003, 20003])
+def test_norm_of_tiny_rows_at_both_ends_of_eps(cols, eps):
+    """The limit of 2^-119 is on |x gain|, whatever eps makes of it: rows below it are zeros though their normed values may be far above, rows from it on keep their codes though
+    their scale may be below fp32's normal numbers or 0.  The scale: as in check_norm, its last product and division off by half of the least subnormal more."""
+    g = gen(cols)
+    x = torch.zeros(7, cols)
+    x[0], x[1], x[2] = TINY / 2, TINY, TINY
+    x[1, 0], x[2, cols - 1] = 0.75 * TINY, -TINY
+    x[3] = 1e-30 * torch.randn(cols, generator=g)
+    x[4] = 1e-15 * torch.randn(cols, generator=g)
+    x[5] = torch.randn(cols, generator=g)
+    x[6, cols // 2] = TINY                                      # halved by the gain
+    gain = torch.ones(cols)
+    gain[cols // 2] = 0.5
+    q = B.Q8(7, cols)
+    q.codes.fill_(55)
+    X = x.cuda()
+    B.op_rmsnorm_q8(X, gain.cuda(), eps, q)
+    n, e32 = x.double() * gain.double(), float(torch.tensor(eps, dtype=F32))
+    want, _ = exact_codes(n)
+    top = n.abs().amax(1)
+    zeros = top < TINY
+    assert zeros.tolist() == [True, False, False, False, False, False, True]
+    assert not codes_of(q)[zeros].any() and not q.scales.cpu()[zeros].any()
+    assert (codes_of(q) - want).abs().max() <= 0.5 + 127 * 4.02 * U
+    scale = torch.where(zeros, torch.zeros(()).double(), top / torch.sqrt((x.double() ** 2).mean(1) + e32) / 127.0)
+    chain = 4 * -(-cols // 1024) + 11
+    assert ((q.scales.cpu().double() - scale).abs() <= scale * (chain / 2 + 8) * U + 1.01 * 2.0 ** -150).all()
+    check_padding(q)
+
+
+@pytest.mark.parametrize("cols", [5, 1003, 20003])
+@pytest.mark.parametrize("gain_type", TYPES)
+def test_norm_of_rows_whose_products_with_the_gain_leave_fp32(cols, gain_type):
+    """1e17 times a gain of 3e38 is no number of fp32, though its norm may be one: a row with an infinity (half's gains are smaller).  The rows beside it do not notice."""
+    top = 65504.0 if gain_type is F16 else 3e38
+    gain = torch.ones(cols).to(gain_type)
+    gain[1] = top
+    x = torch.ones(3, cols)
+    x[1] = 0.0
+    x[1, 1], x[1, 2] = 1e17, 1e18                               # squares 1e36
+    q = B.Q8(3, cols)
+    B.op_rmsnorm_q8(x.cuda(), gain.cuda(), 1e-6, q)
+    bad = torch.tensor([False, gain_type is not F16, False])
+    assert torch.equal(torch.isnan(q.scales.cpu()), bad) and not codes_of(q)[bad].any()
+    ok = B.Q8.of(q.codes[:, :cols][~bad.cuda()].contiguous(), q.scales[~bad.cuda()].contiguous())
+    check_norm(x[~bad], None, gain, 1e-6, ok, x[~bad])
+
+
 @pytest.mark.parametrize("cols", [64, 500, 1003, 2048, 4096, 9000, 12288, 16384, 20003])
 def test_rows_do_not_depend_on_the_rows_beside_them(cols):
     """One row, a hundred and two thousand take different numbers of threads a row: same bits of stream, codes and scales."""
