@@ -392,6 +392,35 @@ def test_gemm_that_begins_anywhere_in_k(epilogue, dtype):
         run_product(M, N, K, epilogue, dtype)
 
 
+# rows, columns, K: tests/test_q8_plan.py: every tile, with weights' rows a multiple of 4 KiB apart
+TURN_SIZES = [(460, 21890, 4000), (386, 22126, 4096), (502, 16502, 4000), (390, 16564, 4000), (391, 8526, 4000), (475, 8758, 4000), (455, 8222, 4000), (400, 8228, 4000),
+              (457, 4140, 4000), (455, 2078, 4000), (481, 1028, 4000), (10, 16764, 4000), (482, 524, 3981), (70, 130, 4000), (341, 3940, 2332), (87, 16420, 2478),
+              (108, 14410, 1929), (512, 24576, 4096), (391, 24576, 4096), (450, 4096, 12288)]
+
+
+@pytest.mark.parametrize("epilogue,dtype", EPILOGUES)
+@pytest.mark.parametrize("M,N,K", TURN_SIZES)
+def test_gemm_that_begins_anywhere_in_k_on_every_tile(M, N, K, epilogue, dtype):
+    """The same on all tiles; rows that are shorter than a multiple of 4 KiB have gaps behind them, whose bytes do not count.  The same bits as with rows that are 128 codes further
+    apart, where every tile begins at K's start."""
+    a, sa, w, sw = operands(M, N, K, 7)
+    width, apart = (K + 127) // 128 * 128, (K + 4095) // 4096 * 4096
+
+    def spread(stride):
+        store = torch.full((N, stride), 99, dtype=torch.int8, device="cuda")
+        store[:, :K], store[:, K:width] = w, 0
+        q = B.Q8(0, K)
+        q._set(store, sw, K)
+        return q
+    cols = N // 2 if epilogue == B.EPI_SWIGLU else N
+    old = torch.randn(M, cols, device="cuda").to(dtype)
+    out, straight, A = old.clone(), old.clone(), B.Q8.of(a, sa)
+    B.op_gemm_q8(epilogue, A, spread(apart), out)
+    check_product(epilogue, dtype, out, old, product(a, sa, w, sw))
+    B.op_gemm_q8(epilogue, A, spread(apart + 128), straight)
+    assert torch.equal(out, straight)
+
+
 @pytest.mark.parametrize("M", [1, 8, 9, 16, 17, 32, 33, 64, 65])
 def test_gemm_around_the_kernel_of_few_rows(M):
     for N, K in ((64, 70), (4096, 1024), (4098, 1024), (8192, 1024), (8194, 1000), (2046, 2176), (2048, 2176), (512, 4224)):

@@ -20,6 +20,8 @@ extern "C" void plan(int M, int cols, int slices, int epi, int *out) {
   out[0] = p.rows_first; out[1] = p.first; out[2] = p.kind; out[3] = kQ8Tile[p.first].bm; out[4] = kQ8Tile[p.kind].bn;
 }
 extern "C" int few(int M, int N, int K) { return q8_few_rows(M, N, K); }
+extern "C" int turn(int M, long long stride) { return q8_turn(M, stride); }
+extern "C" int columns(int kind, int glu) { return glu ? kQ8Tile[kind].bn / 2 : kQ8Tile[kind].bn; }
 """
 
 
@@ -48,6 +50,20 @@ def test_the_gpu_tests_reach_every_tile(plan):
         ragged = set(itertools.chain(*(kinds(plan, M, N * (2 if epilogue == B.EPI_SWIGLU else 1), K, epilogue) for M, N, K in G.ODD_SIZES)))
         want = set(range(plan.tiles())) - ({11, 12} if epilogue == B.EPI_SWIGLU else set())
         assert seen | ragged == want, (epilogue, want - seen - ragged)
+
+
+def test_the_gpu_tests_turn_every_tile(plan):
+    """Loops that begin elsewhere than at K's start, at different places in the tiles of a launch."""
+    for epilogue, _ in G.EPILOGUES:
+        glu, seen = epilogue == B.EPI_SWIGLU, set()
+        for M, N, K in G.TURN_SIZES:
+            turn, slices = plan.turn(M, ctypes.c_longlong(-(-K // 4096) * 4096)), -(-K // 128)
+            assert turn and not plan.turn(M, ctypes.c_longlong(-(-K // 4096) * 4096 + 128))
+            for kind in kinds(plan, M, N, K, epilogue):
+                tiles = -(-(N // 2 if glu else N) // plan.columns(kind, glu))
+                if len({i * turn % slices for i in range(tiles)}) >= min(slices, 3):
+                    seen.add(kind)
+        assert seen == set(range(plan.tiles())) - ({11, 12} if glu else set()), (epilogue, seen)
 
 
 def test_plans_of_all_sizes_are_possible(plan):
