@@ -421,6 +421,31 @@ def test_gemm_that_begins_anywhere_in_k_on_every_tile(M, N, K, epilogue, dtype):
     assert torch.equal(out, straight)
 
 
+@pytest.mark.parametrize("M", [1, 12, 100, 600])
+def test_weights_of_nearly_four_gib(M):
+    """Offsets within the weights pass 31 bits: columns in front of 2 GiB, around it and the last ones, on the kernel of few rows and on small and large tiles."""
+    N, K = 1000000, 4096
+    W = B.Q8(N, K)
+    g = torch.Generator(device="cuda").manual_seed(M)
+    for i in range(0, N, 100000):
+        W.codes[i:i + 100000].random_(-128, 128, generator=g)
+    W.scales.uniform_(1e-5, 1e-4, generator=g)
+    a, sa, _, _ = operands(M, 1, K, 8)
+    A = B.Q8.of(a, sa)
+    old = torch.randn(M, N, device="cuda")
+    out = old.clone()
+    B.op_gemm_q8(B.EPI_RESIDUAL, A, W, out)
+    for at in (0, (1 << 31) // K - 150, N - 300):
+        c = slice(at, at + 300)
+        check_product(B.EPI_RESIDUAL, F32, out[:, c], old[:, c], product(a, sa, W.codes[c], W.scales[c]))
+    del out, old
+    h = torch.empty(M, N // 2, dtype=BF16, device="cuda")
+    B.op_gemm_q8(B.EPI_SWIGLU, A, W, h)
+    for at in (0, (1 << 30) // K, (1 << 31) // K - N // 2, N // 2 - 300):
+        rows = torch.cat([torch.arange(at, at + 300), torch.arange(N // 2 + at, N // 2 + at + 300)]).cuda()
+        check_product(B.EPI_SWIGLU, BF16, h[:, at:at + 300], None, product(a, sa, W.codes[rows], W.scales[rows]))
+
+
 @pytest.mark.parametrize("M", [1, 8, 9, 16, 17, 32, 33, 64, 65])
 def test_gemm_around_the_kernel_of_few_rows(M):
     for N, K in ((64, 70), (4096, 1024), (4098, 1024), (8192, 1024), (8194, 1000), (2046, 2176), (2048, 2176), (512, 4224)):
