@@ -93,6 +93,7 @@ def load_group(which, n, lds_off, m0_at=0):
     offset is added to both (the lane's comes without it)."""
     base, lds, off = ("s[20:21]", "%[la]", "ga") if which == "A" else ("s[22:23]", "%[lb]", "gb")
     m0 = lambda j: f"s_add_u32 m0, {lds}, {lds_off + j // 4 * 4096}\\n s_nop 0\\n " if j % 4 == 0 or j == m0_at else ""
+    # one immediate in two notations: the 8-bit loops' offsets are multiples of 0x400; the 16-bit loops' text is kept as it was measured, to the byte
     at = (lambda j: f"{j % 4 * 1024:#x}") if Q8 else (lambda j: j % 4 * 1024)
     return [f"{m0(j)}global_load_lds_dwordx4 %[{off}{j}], {base} offset:{at(j)}" for j in range(n)]
 
